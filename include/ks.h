@@ -126,6 +126,21 @@ typedef struct {
 
 #define KS_STATIC_MAX_KEYS 524288 /* partial top-k entries ks_select_trees_static can hold  */
 
+/* Types of the elements of the operators' arrays (ks_quantize_e4m3, ks_matmul_e4m3, ks_sample). KS_E4M3 is the eight-bit
+ * type with four exponent and three mantissa bits, no infinities, largest value 448, 0x7F / 0xFF no number. */
+enum { KS_F32 = 0, KS_BF16 = 1, KS_F16 = 2, KS_E4M3 = 3 };
+/* How the scale of a block is stored: fp32, or one byte b that stands for 2^(b - 127) (255: no number). */
+enum { KS_SCALE_F32 = 0, KS_SCALE_E8M0 = 1 };
+#define KS_SCALE_BLOCK 128 /* columns that share a scale */
+
+/* What of a row's distribution ks_sample draws from. 16 bytes. */
+typedef struct {
+  float temperature; /* scores are divided by it; 0: the best candidate alone                */
+  int32_t top_k;     /* the best so many stay; 0: all                                        */
+  float top_p;       /* of those, the fewest best that hold this part of their sum; 1: all   */
+  float min_p;       /* of those, the ones with at least this part of the best one's weight  */
+} ks_sampling;
+
 typedef struct ks_ctx ks_ctx;
 typedef struct ks_model ks_model;
 typedef struct ks_catalogue ks_catalogue;
@@ -341,6 +356,61 @@ ks_status ks_select_host(ks_ctx* ctx, const ks_problem* h_p, int P, const ks_can
  * Asynchronous on `stream`. */
 ks_status ks_merge_topk(ks_ctx* ctx, const int32_t* d_idx, const float* d_score, int P, int n, int k,
                         int32_t* d_topk_idx, float* d_topk_score, void* stream);
+
+/* ---- products of operands held in eight bits, and answers that are drawn ------------------- */
+
+/* Rows of values to e4m3 with a scale for each block of `block_rows` x 128 (1: activations, a scale for each row and 128
+ * columns; 128: weights). With a the block's largest finite magnitude:
+ *   KS_SCALE_E8M0  scale 2^e with the smallest e >= -127 for which a / 2^e <= 448; q = x / 2^e rounded to nearest even
+ *   KS_SCALE_F32   a' = max(a, 2^-100), scale a' / 448; q = x * (448 / a') rounded to nearest even, with the product and both
+ *                  quotients rounded to fp32
+ * so that q times its scale stands for x. What is not finite becomes the code that is no number.
+ *   d_x      device, [rows][cols] of x_type (KS_F32, KS_BF16, KS_F16), rows ldx elements apart (ldx >= cols)
+ *   d_q      device, [rows][cols] bytes, rows ldq bytes apart; 16-byte aligned, ldq a multiple of 16 (as ks_matmul_e4m3 reads
+ *            them); bytes between cols and ldq are left as they are
+ *   d_scale  device, [ceil(rows / block_rows)][ceil(cols / 128)] fp32 or bytes
+ * Asynchronous on `stream`; no workspace. */
+ks_status ks_quantize_e4m3(ks_ctx* ctx, const void* d_x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int block_rows,
+                           int scale_type, uint8_t* d_q, int64_t ldq, void* d_scale, void* stream);
+
+/* d[i][j] = act(sum over blocks b of 128 of sa[i][b] * sb[j / 128][b] * (sum over k in b of a[i][k] * b[j][k]) + bias[j]) for
+ * i < m, j < n, with fp32 sums, rounded once to d_type: a layer on rows held in eight bits with weights [n][k] held in eight
+ * bits. act is the identity or, with `relu`, x for x > 0 and else 0.
+ *   d_a, d_b        device, e4m3, [m][k] and [n][k], rows lda / ldb bytes apart; 16-byte aligned, lda and ldb multiples of 16
+ *   d_a_scale       device, [m][ceil(k / 128)] of scale_type (ks_quantize_e4m3 with block_rows 1)
+ *   d_b_scale       device, [ceil(n / 128)][ceil(k / 128)] of scale_type (block_rows 128)
+ *   d_bias          device, [n] fp32, or NULL
+ *   d_d             device, [m][n] of d_type, rows ldd elements apart. KS_E4M3: quantised as ks_quantize_e4m3 with block_rows 1
+ *                   does the fp32 sums, scales of scale_type to d_d_scale [m][ceil(n / 128)]; d_d and ldd as d_q and ldq there
+ *   d_d_scale       only for KS_E4M3, else NULL
+ * The scales' products sa * sb have to be fp32 numbers; d_d may overlap none of the inputs. m == 0 or n == 0 does nothing;
+ * k == 0 is the empty sum. Asynchronous on `stream`. m, n, k < 2^31. KS_ERR_UNSUPPORTED where a grid would not hold m. */
+ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const void* d_a_scale, const uint8_t* d_b, int64_t ldb,
+                         const void* d_b_scale, int scale_type, int64_t m, int64_t n, int64_t k, const float* d_bias, int relu,
+                         void* d_d, int64_t ldd, int d_type, void* d_d_scale, void* stream);
+
+/* Draws from the softmax of scores, for callers that answer with a distribution rather than with its best candidates (ks_select):
+ * candidates to be measured, a policy that explores. A row's scores x_0 .. x_{c-1} get weights w_j = exp((x_j - max) /
+ * temperature); a score that is not a number counts as -inf, whose weight is 0, and where the largest score is +inf its holders alone have weight, the same each.
+ * In the order (score descending, index ascending) the first top_k stay; of these the shortest front whose weights sum to at
+ * least top_p of theirs (at least one); of these those with w_j >= min_p. With s the sum of what stays, a draw for u in [0, 1) is
+ * the first candidate in the order of the indices up to which the weights that stay sum to more than u s.
+ * Temperature 0: the best candidate (the first of those that share the score), whatever u.
+ *   d_scores       device, score_type KS_F32, KS_BF16 or KS_F16. Without d_seg_offsets row i is [i * ld, i * ld + c), ld >= c; with it
+ *                  (P + 1 non-decreasing entries) row i is [d_seg_offsets[i], d_seg_offsets[i + 1]), at most 2^31 - 1 long, and
+ *                  c and ld are not used
+ *   d_params       device, [P], settings of each row, or NULL: *h_params for all rows. Of d_params a temperature that is not
+ *                  above 0 counts as 0, top_k < 1 as 0, top_p not below 1 as 1, min_p not above 0 as 0
+ *   d_u            device, [P][draws] fp32; below 0 counts as 0, from 1 on as the largest below 1. 1 <= draws <= KS_MAX_K
+ *   d_idx          device, [P][draws]: positions in the row; -1 where every weight is 0 (an empty row, all scores -inf)
+ *   d_logp         device, [P][draws], or NULL: log(w_j / s) of the candidate drawn; -inf beside -1
+ * Weights are held to 2^-52 of the best one's (rows of more than 1,023 scores: to 2^-62 times the power of two above their
+ * number); what lies below half of that is never drawn. Draws do not depend on how the work is shared out: the same call gives the same bits. Asynchronous on
+ * `stream`; no workspace. KS_ERR_INVALID_ARG for draws out of range, a negative size, or *h_params with a setting that is no number,
+ * negative, or top_p outside (0, 1], min_p above 1. */
+ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int c, int64_t ld, const int64_t* d_seg_offsets,
+                    const ks_sampling* h_params, const ks_sampling* d_params, const float* d_u, int draws, int32_t* d_idx,
+                    float* d_logp, void* stream);
 
 /* ---- selection without any allocation ------------------------------------------------------- */
 

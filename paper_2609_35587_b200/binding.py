@@ -29,7 +29,13 @@ EXPORTS = ("ks_create", "ks_destroy", "ks_last_cuda_error", "ks_model_create_gbd
            "ks_select_one_prepared",
            "ks_debug_set_wait", "ks_debug_bounds_line", "ks_debug_bounds_clear", "ks_debug_walk_floor", "ks_debug_class_walks",
            "ks_debug_split_walks",
-           "ks_debug_limit_workspace")
+           "ks_debug_limit_workspace", "ks_quantize_e4m3", "ks_matmul_e4m3", "ks_sample")
+KS_F32, KS_BF16, KS_F16, KS_E4M3 = range(4)
+KS_SCALE_F32, KS_SCALE_E8M0 = 0, 1
+KS_SCALE_BLOCK = 128
+_TYPES = {torch.float32: KS_F32, torch.bfloat16: KS_BF16, torch.float16: KS_F16, torch.float8_e4m3fn: KS_E4M3}
+_SCALES = {"f32": (KS_SCALE_F32, torch.float32), "e8m0": (KS_SCALE_E8M0, torch.float8_e8m0fnu)}
+SAMPLING_DT = np.dtype([("temperature", "<f4"), ("top_k", "<i4"), ("top_p", "<f4"), ("min_p", "<f4")])
 
 
 class KsError(RuntimeError):
@@ -43,6 +49,11 @@ class _Problem(ctypes.Structure):
     _fields_ = [("m", ctypes.c_uint32), ("n", ctypes.c_uint32), ("k", ctypes.c_uint32),
                 ("layout", ctypes.c_uint8), ("dtype_ab", ctypes.c_uint8),
                 ("dtype_d", ctypes.c_uint8), ("epi_flags", ctypes.c_uint8)]
+
+
+class _Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int32), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float)]
 
 
 def _load() -> ctypes.CDLL:
@@ -91,6 +102,9 @@ def _load() -> ctypes.CDLL:
     lib.ks_debug_class_walks.restype = i64
     lib.ks_debug_split_walks.argtypes = [vp]
     lib.ks_debug_split_walks.restype = i64
+    lib.ks_quantize_e4m3.argtypes = [vp, vp, i32, i64, i64, i64, i32, i32, vp, i64, vp, vp]
+    lib.ks_matmul_e4m3.argtypes = [vp, vp, i64, vp, vp, i64, vp, i32, i64, i64, i64, vp, i32, vp, i64, i32, vp, vp]
+    lib.ks_sample.argtypes = [vp, vp, i32, i32, i32, i64, vp, ctypes.POINTER(_Sampling), vp, vp, i32, vp, vp, vp]
     lib.ks_debug_bounds_line.restype = i32
     lib.ks_debug_bounds_clear.restype = None
     for name in EXPORTS:
@@ -122,6 +136,21 @@ def _dptr(t):
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("expected a contiguous CUDA tensor")
     return ctypes.c_void_p(t.data_ptr())
+
+
+def _rows(t, what):
+    """Pointer and row stride (elements) of a matrix whose rows may be padded."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: expected a CUDA matrix with contiguous rows")
+    # (torch gives a single row, or one of no columns, any stride)
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _empty_e4m3(rows, cols, device):
+    """[rows, cols] e4m3 whose rows begin on 16-byte boundaries."""
+    wide = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
+    return wide[:, :cols]
 
 
 def _hptr(a):
@@ -444,6 +473,86 @@ class Context:
                                  _stream())
         self._check(st, "ks_select_host")
         return h_idx, h_score
+
+    # ---- products of operands held in eight bits, and answers that are drawn ------------------
+    def quantize_e4m3(self, x, block_rows: int = 1, scale: str = "e8m0", out=None, out_scale=None):
+        """Rows of fp32 / bf16 / fp16 values to e4m3 with a scale ("e8m0" or "f32") for each block of
+        block_rows (1 or 128) x 128. Returns (q, scales); the rows of q begin on 16-byte boundaries."""
+        rows, cols = x.shape
+        st, dtype = _SCALES[scale]
+        br = max(int(block_rows), 1)  # an invalid one is reported by the library, not by torch
+        if out is None:
+            out = _empty_e4m3(rows, cols, self.device)
+        if out_scale is None:
+            out_scale = torch.empty(((rows + br - 1) // br, (cols + 127) // 128), dtype=dtype, device=self.device)
+        if x.dtype not in _TYPES or out.dtype != torch.float8_e4m3fn or out_scale.dtype != dtype:
+            raise ValueError("quantize_e4m3: element types")
+        if out.shape != x.shape or out_scale.shape != ((rows + br - 1) // br, (cols + 127) // 128):
+            raise ValueError("quantize_e4m3: shapes of the results")
+        xp, ldx = _rows(x, "x")
+        qp, ldq = _rows(out, "out")
+        self._check(_lib.ks_quantize_e4m3(self._h, xp, _TYPES[x.dtype], rows, cols, ldx, int(block_rows), st, qp,
+                                          ldq, _dptr(out_scale), _stream()), "ks_quantize_e4m3")
+        return out, out_scale
+
+    def matmul_e4m3(self, a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=torch.bfloat16, out=None,
+                    out_scale=None):
+        """a [m, k] times the transpose of b [n, k], both as quantize_e4m3 makes them (b with block_rows 128).
+        Returns [m, n] of out_dtype; for torch.float8_e4m3fn (q, scales) with a scale for each row and 128 columns."""
+        (m, k), (n, kb) = a.shape, b.shape
+        blocks = (k + 127) // 128
+        if kb != k or a.dtype != torch.float8_e4m3fn or b.dtype != torch.float8_e4m3fn:
+            raise ValueError("matmul_e4m3: operands")
+        if a_scale.dtype != b_scale.dtype or a_scale.dtype not in (torch.float32, torch.float8_e8m0fnu):
+            raise ValueError("matmul_e4m3: types of the scales")
+        if a_scale.shape != (m, blocks) or b_scale.shape != ((n + 127) // 128, blocks):
+            raise ValueError("matmul_e4m3: shapes of the scales")
+        if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
+            raise ValueError("matmul_e4m3: bias")
+        quantised = out_dtype == torch.float8_e4m3fn
+        if out is None:
+            out = _empty_e4m3(m, n, self.device) if quantised else torch.empty((m, n), dtype=out_dtype, device=self.device)
+        if quantised and out_scale is None:
+            out_scale = torch.empty((m, (n + 127) // 128), dtype=a_scale.dtype, device=self.device)
+        if out.shape != (m, n) or out.dtype != out_dtype or out_dtype not in _TYPES or quantised != (out_scale is not None):
+            raise ValueError("matmul_e4m3: result")
+        if quantised and (out_scale.dtype != a_scale.dtype or out_scale.shape != (m, (n + 127) // 128)):
+            raise ValueError("matmul_e4m3: scales of the result")
+        (ap, lda), (bp, ldb), (op, ldd) = _rows(a, "a"), _rows(b, "b"), _rows(out, "out")
+        st = KS_SCALE_F32 if a_scale.dtype == torch.float32 else KS_SCALE_E8M0
+        self._check(_lib.ks_matmul_e4m3(self._h, ap, lda, _dptr(a_scale), bp, ldb, _dptr(b_scale), st, m, n, k,
+                                        _dptr(bias), int(relu), op, ldd, _TYPES[out_dtype], _dptr(out_scale), _stream()),
+                    "ks_matmul_e4m3")
+        return (out, out_scale) if quantised else out
+
+    def sample(self, scores, u, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
+               params=None, d_seg_off=None, out_idx=None, out_logp=None):
+        """Draws from the softmax of scores ([P, C], or flat with the P + 1 offsets d_seg_off) for the given random
+        numbers u [P, draws]. `params`: [P] SAMPLING_DT records on the device (to_device), settings of each row
+        instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each."""
+        P, draws = u.shape
+        if u.dtype != torch.float32 or scores.dtype not in _TYPES:
+            raise ValueError("sample: element types")
+        if d_seg_off is None:
+            if scores.shape[0] != P:
+                raise ValueError("sample: a row of scores for each row of u")
+            sp, ld = _rows(scores, "scores")
+            c = scores.shape[1]
+        else:
+            if d_seg_off.dtype != torch.int64 or d_seg_off.shape != (P + 1,):
+                raise ValueError("sample: d_seg_off")
+            sp, ld, c = _dptr(scores), 0, 0
+        if params is not None and params.numel() * params.element_size() != 16 * P:
+            raise ValueError("sample: params")
+        if out_idx is None:
+            out_idx = torch.empty((P, draws), dtype=torch.int32, device=self.device)
+            out_logp = torch.empty((P, draws), dtype=torch.float32, device=self.device)
+        if out_idx.shape != u.shape or (out_logp is not None and out_logp.shape != u.shape):
+            raise ValueError("sample: shapes of the results")
+        one = _Sampling(float(temperature), int(top_k), float(top_p), float(min_p))
+        self._check(_lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, _dptr(d_seg_off), ctypes.byref(one),
+                                   _dptr(params), _dptr(u), draws, _dptr(out_idx), _dptr(out_logp), _stream()), "ks_sample")
+        return out_idx, out_logp
 
     # ---- search space and validity ----------------------------------------------------------
     def enumerate(self, first: int, count: int, out=None):

@@ -223,6 +223,9 @@ ks_status check_pairs(int P, int C, const void* seg_off, const void* seg_idx, in
 
 // problem and candidate records are fetched with 128-bit loads
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+constexpr int64_t kMaxExtent = INT32_MAX;  // of the arrays of the eight-bit operators
 
 }  // namespace
 
@@ -834,6 +837,61 @@ ks_status ks_select_one_prepared(ks_ctx* ctx, const ks_catalogue* cat, ks_proble
   std::memcpy(h_topk_idx, pin_idx, k * sizeof(int32_t));
   std::memcpy(h_topk_score, pin_sc, k * sizeof(float));
   return KS_OK;
+}
+
+ks_status ks_quantize_e4m3(ks_ctx* ctx, const void* d_x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int block_rows,
+                           int scale_type, uint8_t* d_q, int64_t ldq, void* d_scale, void* stream) {
+  if (!ctx || rows < 0 || cols < 0 || rows > kMaxExtent || cols > kMaxExtent || ldx < cols || ldq < cols || ldq % 16)
+    return KS_ERR_INVALID_ARG;
+  if (x_type < KS_F32 || x_type > KS_F16 || (block_rows != 1 && block_rows != KS_SCALE_BLOCK)) return KS_ERR_INVALID_ARG;
+  if (scale_type != KS_SCALE_F32 && scale_type != KS_SCALE_E8M0) return KS_ERR_INVALID_ARG;
+  if (rows == 0 || cols == 0) return KS_OK;
+  if (!d_x || !d_q || !d_scale || !aligned16(d_q)) return KS_ERR_INVALID_ARG;
+  if (!aligned(d_x, x_type == KS_F32 ? 4 : 2) || (scale_type == KS_SCALE_F32 && !aligned(d_scale, 4))) return KS_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  cudaError_t e = ks::launch_quantize_e4m3(d_x, x_type, rows, cols, ldx, block_rows, scale_type, d_q, ldq, d_scale,
+                                           static_cast<cudaStream_t>(stream), &ctx->launches);
+  if (e == cudaErrorInvalidConfiguration) return KS_ERR_UNSUPPORTED;
+  return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_quantize_e4m3");
+}
+
+ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const void* d_a_scale, const uint8_t* d_b, int64_t ldb,
+                         const void* d_b_scale, int scale_type, int64_t m, int64_t n, int64_t k, const float* d_bias, int relu,
+                         void* d_d, int64_t ldd, int d_type, void* d_d_scale, void* stream) {
+  if (!ctx || m < 0 || n < 0 || k < 0 || m > kMaxExtent || n > kMaxExtent || k > kMaxExtent) return KS_ERR_INVALID_ARG;
+  if (lda < k || ldb < k || ldd < n || lda % 16 || ldb % 16) return KS_ERR_INVALID_ARG;
+  if (scale_type != KS_SCALE_F32 && scale_type != KS_SCALE_E8M0) return KS_ERR_INVALID_ARG;
+  if (d_type < KS_F32 || d_type > KS_E4M3 || (d_type == KS_E4M3) != (d_d_scale != nullptr)) return KS_ERR_INVALID_ARG;
+  if (m == 0 || n == 0) return KS_OK;
+  if (!d_d || (k > 0 && (!d_a || !d_b || !d_a_scale || !d_b_scale))) return KS_ERR_INVALID_ARG;
+  if (!aligned16(d_a) || !aligned16(d_b) || !aligned(d_bias, 4)) return KS_ERR_INVALID_ARG;
+  if (scale_type == KS_SCALE_F32 && (!aligned(d_a_scale, 4) || !aligned(d_b_scale, 4) || !aligned(d_d_scale, 4))) return KS_ERR_INVALID_ARG;
+  if (d_type == KS_E4M3 ? (!aligned16(d_d) || ldd % 16) : !aligned(d_d, d_type == KS_F32 ? 4 : 2)) return KS_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  const ks::MatmulE4m3 p{d_a, lda, d_a_scale, d_b, ldb, d_b_scale, scale_type, m, n, k, d_bias, relu != 0,
+                         d_d, ldd, d_type, d_d_scale};
+  cudaError_t e = ks::launch_matmul_e4m3(p, ctx->d_status, static_cast<cudaStream_t>(stream), &ctx->launches, &ctx->wait);
+  if (e == cudaErrorInvalidConfiguration) return KS_ERR_UNSUPPORTED;
+  return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_matmul_e4m3");
+}
+
+ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int c, int64_t ld, const int64_t* d_seg_offsets,
+                    const ks_sampling* h_params, const ks_sampling* d_params, const float* d_u, int draws, int32_t* d_idx,
+                    float* d_logp, void* stream) {
+  if (!ctx || P < 0 || draws < 1 || draws > KS_MAX_K || score_type < KS_F32 || score_type > KS_F16) return KS_ERR_INVALID_ARG;
+  if (!d_seg_offsets && (c < 0 || ld < c)) return KS_ERR_INVALID_ARG;
+  if (!d_params) {  // (comparisons that a value that is no number does not pass)
+    if (!h_params || !(h_params->temperature >= 0.0f) || !std::isfinite(h_params->temperature) || h_params->top_k < 0 ||
+        !(h_params->top_p > 0.0f && h_params->top_p <= 1.0f) || !(h_params->min_p >= 0.0f && h_params->min_p <= 1.0f))
+      return KS_ERR_INVALID_ARG;
+  }
+  if (P == 0) return KS_OK;
+  if (!d_u || !d_idx || (!d_scores && (d_seg_offsets || c > 0))) return KS_ERR_INVALID_ARG;
+  if (!aligned(d_scores, score_type == KS_F32 ? 4 : 2) || !aligned(d_params, 4) || !aligned(d_seg_offsets, 8)) return KS_ERR_INVALID_ARG;
+  DeviceGuard g(ctx->device);
+  const ks::SampleArgs a{d_scores, ld, d_seg_offsets, P, c, d_params ? ks_sampling{} : *h_params, d_params, d_u, draws, d_idx, d_logp};
+  cudaError_t e = ks::launch_sample(a, score_type, static_cast<cudaStream_t>(stream), &ctx->launches);
+  return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_sample");
 }
 
 ks_status ks_select_host(ks_ctx* ctx, const ks_problem* h_p, int P, const ks_candidate* h_c, int C,

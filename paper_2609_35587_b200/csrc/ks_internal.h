@@ -348,6 +348,41 @@ size_t score_wide_scratch_bytes(const MlpModel& m, int64_t rows, bool lean);
 cudaError_t launch_score_wide(const MlpModel& m, const float* d_feat, int64_t rows, float* d_scores, void* scratch,
                               int* status, cudaStream_t stream, int64_t* launches, const FastWait* wait);
 
+// Operators on eight-bit operands and draws (ks_quant.cu, ks_matmul8.cu, ks_sample.cu).
+cudaError_t launch_quantize_e4m3(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int block_rows,
+                                 int scale_type, uint8_t* q, int64_t ldq, void* scale, cudaStream_t stream, int64_t* launches);
+struct MatmulE4m3 {
+  const uint8_t* a;
+  int64_t lda;
+  const void* a_scale;
+  const uint8_t* b;
+  int64_t ldb;
+  const void* b_scale;
+  int scale_type;
+  int64_t m, n, k;
+  const float* bias;
+  int relu;
+  void* d;
+  int64_t ldd;
+  int d_type;
+  void* d_scale;
+};
+cudaError_t launch_matmul_e4m3(const MatmulE4m3& p, int* status, cudaStream_t stream, int64_t* launches, const FastWait* wait);
+struct SampleArgs {
+  const void* scores;
+  int64_t ld;
+  const int64_t* seg_off;
+  int64_t p;
+  int c;
+  ks_sampling all;
+  const ks_sampling* params;
+  const float* u;
+  int draws;
+  int32_t* idx;
+  float* logp;
+};
+cudaError_t launch_sample(const SampleArgs& a, int score_type, cudaStream_t stream, int64_t* launches);
+
 // k-way merge of gathered partial lists (multi-GPU candidate split).
 cudaError_t launch_merge_lists(const int32_t* d_idx, const float* d_score, int P, int n, int k, int32_t* d_out_idx,
                                float* d_out_score, cudaStream_t stream, int64_t* launches);
