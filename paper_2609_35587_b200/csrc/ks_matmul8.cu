@@ -1,110 +1,693 @@
 // Product of two operands held in e4m3 with a scale for each block of 128 (ks_matmul_e4m3).
 //
 // d[m][n] = sum over blocks b of sa[m][b] * sb[n / 128][b] * (sum over k in b of a[m][k] * b[n][k]): the sum within a block
-// is plain, so that the scales come in once per block and not once per element.
-#include <cuda_fp8.h>
+// is plain, so that the scales come in once per block. A tensor core makes a block's sums (128 of K, four MMAs of 32) into one
+// of two accumulators, the epilogue's threads read them and add them, scaled, to fp32 sums in their registers, while the other
+// accumulator is filled. So the sums of blocks are added with rounding, not with the tensor core's truncation, and scales of
+// any value cost the same.
+#include <cuda.h>
 
 #include <algorithm>
+#include <cstring>
 
 #include "ks_e4m3.cuh"
 #include "ks_internal.h"
+#include "ks_tcgen.cuh"
 
 namespace ks {
 namespace {
 
-constexpr int kRows = 32, kCols = kScaleBlock, kStep = 32, kThreads = 256;
+using Wide = unsigned long long;
 
-__device__ __forceinline__ float e4m3_value(uint8_t v) {
-  return __half2float(__half(__nv_cvt_fp8_to_halfraw(v, __NV_E4M3)));
-}
+constexpr int kSms = 148;  // of the one device this library is built for
 
 __device__ __forceinline__ float scale_value(const void* s, int64_t at, int type) {
-  return type == KS_SCALE_E8M0 ? e8m0_value(static_cast<const uint8_t*>(s)[at]) : static_cast<const float*>(s)[at];
+  return type == KS_SCALE_E8M0 ? e8m0_value(__ldg(static_cast<const uint8_t*>(s) + at)) : __ldg(static_cast<const float*>(s) + at);
 }
 
-// A CTA makes 32 rows x 128 columns: a warp four rows, a lane every 32nd column of them, so that a row's 128 columns, the
-// block of a quantised result, lie in one warp.
-__global__ void __launch_bounds__(kThreads) matmul_kernel(const __grid_constant__ MatmulE4m3 p) {
-  __shared__ float s_a[kRows][kStep + 1], s_b[kCols][kStep + 1];
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int64_t m0 = static_cast<int64_t>(blockIdx.y) * kRows, n0 = static_cast<int64_t>(blockIdx.x) * kCols;
-  const int64_t kb = scale_blocks(p.k);
-  float sum[4][4] = {};
-  for (int64_t b = 0; b < kb; ++b) {
-    float part[4][4] = {};
-    for (int64_t k0 = b * kScaleBlock; k0 < p.k && k0 < (b + 1) * kScaleBlock; k0 += kStep) {
-      __syncthreads();
-      for (int i = threadIdx.x; i < kRows * kStep; i += kThreads) {
-        const int64_t m = m0 + i / kStep, k = k0 + i % kStep;
-        s_a[i / kStep][i % kStep] = m < p.m && k < p.k ? e4m3_value(p.a[m * p.lda + k]) : 0.0f;
-      }
-      for (int i = threadIdx.x; i < kCols * kStep; i += kThreads) {
-        const int64_t n = n0 + i / kStep, k = k0 + i % kStep;
-        s_b[i / kStep][i % kStep] = n < p.n && k < p.k ? e4m3_value(p.b[n * p.ldb + k]) : 0.0f;
-      }
-      __syncthreads();
-      for (int k = 0; k < kStep; ++k)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) part[i][j] = fmaf(s_a[warp * 4 + i][k], s_b[lane + 32 * j][k], part[i][j]);
-    }
-    const float sb = scale_value(p.b_scale, static_cast<int64_t>(blockIdx.x) * kb + b, p.scale_type);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t m = m0 + warp * 4 + i;
-      const float s = m < p.m ? scale_value(p.a_scale, m * kb + b, p.scale_type) * sb : 0.0f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) sum[i][j] = fmaf(part[i][j], s, sum[i][j]);
-    }
+// sum += value * s for two neighbours
+__device__ __forceinline__ void add_scaled(Wide& sum, uint32_t lo, uint32_t hi, Wide s) {
+  asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %0;\n}\n" : "+l"(sum) : "r"(lo), "r"(hi), "l"(s));
+}
+__device__ __forceinline__ Wide both(float v) {
+  const uint32_t u = __float_as_uint(v);
+  return (static_cast<Wide>(u) << 32) | u;
+}
+__device__ __forceinline__ float low(Wide v) { return __uint_as_float(static_cast<uint32_t>(v)); }
+__device__ __forceinline__ float high(Wide v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
+
+// D fp32, A and B e4m3, K-major
+__host__ __device__ constexpr uint32_t instr_desc(int m, int n) {
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+template <int kPair>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  if (kPair)
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// box of [rows][128 of K]; completes on a barrier of either CTA of the pair, or of this CTA
+__device__ __forceinline__ void load_pair(uint32_t dst, const CUtensorMap* map, int k, int row, uint32_t cluster_bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 "
+      "[%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(k), "r"(row), "r"(cluster_bar)
+      : "memory");
+}
+__device__ __forceinline__ void load_one(uint32_t dst, const CUtensorMap* map, int k, int row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(k), "r"(row), "r"(bar)
+      : "memory");
+}
+
+struct MatmulArgs {
+  const void *a_scale, *b_scale;
+  int scale_type;
+  int m, n, kblocks;
+  const float* bias;
+  int relu;
+  void* d;
+  int64_t ldd;
+  int wide_rows;  // rows of d begin on 32-byte boundaries
+  void* d_scale;
+  int wait_limit, starve;
+  int* status;
+};
+
+// Value of an element of the result before it is rounded.
+__device__ __forceinline__ float finish(const MatmulArgs& p, float v, int n) {
+  if (p.bias) v += __ldg(p.bias + n);
+  if (p.relu) v = v > 0.0f ? v : 0.0f;
+  return v;
+}
+
+template <int kType>
+__device__ __forceinline__ void store_one(const MatmulArgs& p, int64_t at, float v) {
+  if (kType == KS_F32) static_cast<float*>(p.d)[at] = v;
+  else if (kType == KS_BF16) static_cast<__nv_bfloat16*>(p.d)[at] = __float2bfloat16_rn(v);
+  else if (kType == KS_F16) static_cast<__half*>(p.d)[at] = __float2half_rn(v);
+  else static_cast<uint8_t*>(p.d)[at] = static_cast<uint8_t>(e4m3_pair(v, 0.0f));
+}
+
+template <int kType>
+__device__ __forceinline__ uint32_t pack(const float* v) {  // four bytes of the result
+  if (kType == KS_F32) return __float_as_uint(v[0]);
+  if (kType == KS_BF16) {
+    const __nv_bfloat162 t = __floats2bfloat162_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&t);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t m = m0 + warp * 4 + i;
-    if (m >= p.m) continue;
-    float amax = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + lane + 32 * j;
-      if (n < p.n && p.bias) sum[i][j] += p.bias[n];
-      if (p.relu) sum[i][j] = sum[i][j] > 0.0f ? sum[i][j] : 0.0f;
-      if (n < p.n) amax = fmaxf(amax, finite_abs(sum[i][j]));
+  if (kType == KS_F16) {
+    const __half2 t = __floats2half2_rn(v[0], v[1]);
+    return *reinterpret_cast<const uint32_t*>(&t);
+  }
+  return e4m3_quad(v[0], v[1], v[2], v[3]);
+}
+template <int kType> constexpr int kBytes = kType == KS_F32 ? 4 : kType == KS_E4M3 ? 1 : 2;
+
+__device__ __forceinline__ float stored_scale(const MatmulArgs& p, float amax, int64_t at, bool write) {
+  uint32_t stored;
+  if (p.scale_type == KS_SCALE_E8M0) {
+    const float inv = block_scale<true>(amax, stored);
+    if (write) static_cast<uint8_t*>(p.d_scale)[at] = static_cast<uint8_t>(stored);
+    return inv;
+  }
+  const float inv = block_scale<false>(amax, stored);
+  if (write) static_cast<uint32_t*>(p.d_scale)[at] = stored;
+  return inv;
+}
+
+// ------------------------------------------------------------------------------------------
+// many rows: pairs of CTAs, 256 x 256 of the result at a time
+// ------------------------------------------------------------------------------------------
+
+constexpr int kThreads = 384;  // warp 0 loads, warp 1 issues MMAs, warps 4..11 are the epilogue
+constexpr int kRegs = 168, kRegsFew = 56, kRegsEpilogue = 224;  // a thread's registers at launch, and after the split
+static_assert(128 * kRegsFew + 256 * kRegsEpilogue <= kThreads * kRegs, "the split hands out what the block was launched with");
+constexpr int kTile = 256, kHalf = kTile / 2;
+constexpr int kStages = 6;
+constexpr int kOperandBytes = kHalf * kScaleBlock;  // a CTA's 128 rows of A, or its half of B's
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kStoreFloats = 32 * 33;  // of a warp, for results whose rows do not begin on 32-byte boundaries
+constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStoreFloats * 4;
+constexpr int kGroup = 8;  // row tiles that share a stretch of column tiles, for L2
+
+struct Tile {
+  int m, n;
+};
+__device__ __forceinline__ Tile tile_at(int64_t t, int tiles_m, int tiles_n) {
+  const int64_t per = static_cast<int64_t>(kGroup) * tiles_n;
+  const int first = static_cast<int>(t / per) * kGroup;
+  const int rows = tiles_m - first < kGroup ? tiles_m - first : kGroup;
+  const int in = static_cast<int>(t % per);
+  return Tile{(first + in % rows) * kTile, (in / rows) * kTile};
+}
+
+template <int kType>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
+                   const __grid_constant__ CUtensorMap map_b) {
+  extern __shared__ unsigned char smem_raw[];
+  // full[kStages] (the leader's are used), empty[kStages], accumulator full[2] and read out[2] (the leader's)
+  __shared__ __align__(8) Wide s_bar[2 * kStages + 4];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = blockIdx.x & 1;  // CTA of the pair; 0 issues the MMAs
+  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_addr(smem), bar0 = smem_addr(&s_bar[0]);
+  auto bar_full = [&](int s) { return bar0 + 8u * s; };
+  auto bar_empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+  auto bar_acc = [&](int i) { return bar0 + 8u * (2 * kStages + i); };
+  auto bar_read = [&](int i) { return bar0 + 8u * (2 * kStages + 2 + i); };
+
+  if (tid == 0) {
+    s_fail = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(bar_full(s), 1);
+      bar_init(bar_empty(s), 1);
     }
-    float inv = 1.0f;
-    if (p.d_type == KS_E4M3) {
-#pragma unroll
-      for (int d = 1; d < 32; d *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
-      uint32_t stored;
-      inv = p.scale_type == KS_SCALE_E8M0 ? block_scale<true>(amax, stored) : block_scale<false>(amax, stored);
-      const int64_t at = m * scale_blocks(p.n) + blockIdx.x;
+    for (int i = 0; i < 2; ++i) {
+      bar_init(bar_acc(i), 1);
+      bar_init(bar_read(i), 16);  // eight epilogue warps of each CTA
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  cluster_sync();  // both CTAs' barriers exist before either is used
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
+  const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
+  volatile int* v_fail = &s_fail;
+
+  // Bounded wait; after the first that runs out every role of the CTA leaves its loop, and the pair's other CTA runs into
+  // its own limit.
+  auto wait_ok = [&](uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < p.wait_limit; ++i) {
+      if (bar_try_tmem(bar, parity)) return true;
+      if ((i & 63) == 63 && *v_fail) return false;
+    }
+    *v_fail = 1;
+    if (p.status) atomicExch(p.status, KS_ERR_TIMEOUT);
+    return false;
+  };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0) {
       if (lane == 0) {
-        if (p.scale_type == KS_SCALE_E8M0) static_cast<uint8_t*>(p.d_scale)[at] = static_cast<uint8_t>(stored);
-        else static_cast<uint32_t*>(p.d_scale)[at] = stored;
+        uint32_t it = 0;
+        bool ok = true;
+        for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+          const Tile at = tile_at(t, tiles_m, tiles_n);
+          for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+            const int s = static_cast<int>(it % kStages);
+            if (!(ok = wait_ok(bar_empty(s), ((it / kStages) & 1u) ^ 1u))) break;
+            const uint32_t full = to_cluster(bar_full(s), 0), dst = sbase + s * kStageBytes;
+            if (rank == 0) bar_expect(bar_full(s), 2u * kStageBytes);
+            if (p.starve) continue;  // test hook: without the copies the waits on this barrier run out
+            load_pair(dst, &map_a, kb * kScaleBlock, at.m + static_cast<int>(rank) * kHalf, full);
+            load_pair(dst + kOperandBytes, &map_b, kb * kScaleBlock, at.n + static_cast<int>(rank) * kHalf, full);
+          }
+        }
       }
-    }
+      __syncwarp();
+    } else if (warp == 1) {
+      if (rank == 0 && lane == 0) {
+        uint32_t it = 0;
+        bool ok = true;
+        constexpr uint32_t idesc = instr_desc(kTile, kTile);
+        for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+          for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+            const uint32_t acc = it & 1u;
+            const int s = static_cast<int>(it % kStages);
+            if (!(ok = wait_ok(bar_read(acc), ((it >> 1) & 1u) ^ 1u) && wait_ok(bar_full(s), (it / kStages) & 1u))) break;
+            fence_after();
+            const uint64_t da = operand_desc(sbase + s * kStageBytes), db = operand_desc(sbase + s * kStageBytes + kOperandBytes);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t n = n0 + lane + 32 * j, at = m * p.ldd + n;
-      if (n >= p.n) continue;
-      const float v = sum[i][j];
-      switch (p.d_type) {
-        case KS_F32: static_cast<float*>(p.d)[at] = v; break;
-        case KS_BF16: static_cast<__nv_bfloat16*>(p.d)[at] = __float2bfloat16_rn(v); break;
-        case KS_F16: static_cast<__half*>(p.d)[at] = __float2half_rn(v); break;
-        default: static_cast<uint8_t*>(p.d)[at] = static_cast<uint8_t>(e4m3_pair(v * inv, 0.0f));
+            for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
+              mma<1>(tmem + acc * kTile, da + 2u * k, db + 2u * k, idesc, k > 0);
+            commit_pair(bar_empty(s));
+            commit_pair(bar_acc(acc));
+          }
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
+    // warp w owns lanes 32 (w % 4) .. and one half of a tile's columns: 128, a block of the result's and of the weights' scales
+    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    const int trow = quarter * 32 + lane;
+    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * kHalf;
+    float* s_store = reinterpret_cast<float*>(smem + kStages * kStageBytes) + (warp - 4) * kStoreFloats;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+      const Tile at = tile_at(t, tiles_m, tiles_n);
+      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + half * kHalf;
+      const bool inside = n0 < p.n;  // (of the warp's columns any)
+      const int64_t sa_at = static_cast<int64_t>(row < p.m ? row : p.m - 1) * p.kblocks;
+      const int64_t sb_at = static_cast<int64_t>(inside ? n0 / kScaleBlock : 0) * p.kblocks;
+      Wide sum[kHalf / 2];
+#pragma unroll
+      for (int q = 0; q < kHalf / 2; ++q) sum[q] = 0;
+      float sa = 0.0f, sb = 0.0f;
+      if (p.kblocks > 0) {
+        sa = scale_value(p.a_scale, sa_at, p.scale_type);
+        sb = scale_value(p.b_scale, sb_at, p.scale_type);
+      }
+      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+        const uint32_t acc = it & 1u;
+        const Wide s = both(sa * sb);
+        if (kb + 1 < p.kblocks) {  // on their way while the accumulator is waited for
+          sa = scale_value(p.a_scale, sa_at + kb + 1, p.scale_type);
+          sb = scale_value(p.b_scale, sb_at + kb + 1, p.scale_type);
+        }
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it >> 1) & 1u)))) break;
+        fence_after();
+        if (inside) {
+          uint32_t r[2][32];
+          tmem_ld32(tmem_mine + acc * kTile, r[0]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tmem_wait(r[c & 1]);
+            if (c < 3) {
+              tmem_ld32(tmem_mine + acc * kTile + 32 * (c + 1), r[(c + 1) & 1]);
+            } else {
+              fence_before();
+              if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
+            }
+#pragma unroll
+            for (int q = 0; q < 16; ++q) add_scaled(sum[16 * c + q], r[c & 1][2 * q], r[c & 1][2 * q + 1], s);
+          }
+        } else {
+          fence_before();
+          if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
+        }
+      }
+      if (!ok || !inside) continue;
+      float inv = 1.0f;
+      if (kType == KS_E4M3) {
+        float amax = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kHalf / 2; ++q) {
+          const int n = n0 + 2 * q;
+          float lo = 0.0f, hi = 0.0f;
+          if (n < p.n) lo = finish(p, low(sum[q]), n);
+          if (n + 1 < p.n) hi = finish(p, high(sum[q]), n + 1);
+          amax = fmaxf(amax, fmaxf(finite_abs(lo), finite_abs(hi)));
+          sum[q] = (static_cast<Wide>(__float_as_uint(hi)) << 32) | __float_as_uint(lo);
+        }
+        inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock, row < p.m);
+      }
+      constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
+      if (p.wide_rows && n0 + kHalf <= p.n) {
+        char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row) * p.ldd + n0) * kBytes<kType>;
+#pragma unroll
+        for (int g = 0; g < kHalf / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
+          uint32_t w[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+              const int c = (g * 8 + i) * kPer + e;
+              const float x = c & 1 ? high(sum[c / 2]) : low(sum[c / 2]);
+              v[e] = kType == KS_E4M3 ? x * inv : finish(p, x, n0 + c);
+            }
+            w[i] = pack<kType>(v);
+          }
+          if (row < p.m)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 32 * g), "r"(w[0]), "r"(w[1]),
+                         "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                         : "memory");
+        }
+      } else {
+        // through shared memory, so that neighbouring threads write neighbouring elements of a row
+#pragma unroll
+        for (int c0 = 0; c0 < kHalf; c0 += 32) {
+          if (n0 + c0 >= p.n) break;
+          __syncwarp();
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            s_store[lane * 33 + 2 * q] = low(sum[c0 / 2 + q]) * inv;
+            s_store[lane * 33 + 2 * q + 1] = high(sum[c0 / 2 + q]) * inv;
+          }
+          __syncwarp();
+          const int n = n0 + c0 + lane, row0 = row - lane;
+          if (n < p.n)
+            for (int r = 0; r < 32 && row0 + r < p.m; ++r) {
+              const float x = s_store[r * 33 + lane];
+              store_one<kType>(p, static_cast<int64_t>(row0 + r) * p.ldd + n, kType == KS_E4M3 ? x : finish(p, x, n));
+            }
+        }
       }
     }
   }
+  // after a failure: time for the copies and MMAs in flight to end
+  if (*v_fail)
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+  __syncthreads();
+  cluster_sync();
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
+// few rows: a CTA takes 128 rows of the weights and a part of K
+// ------------------------------------------------------------------------------------------
+
+// The weights are the MMA's 128 rows and the few rows its columns, so that a CTA reads 16 KB of weights for a block of K
+// whatever m is. The CTAs of a cluster share out K; their sums meet in shared memory, added in the order of the parts, so
+// that the result's bits do not depend on timing.
+constexpr int kFewThreads = 256;  // warp 0 loads, warp 1 issues MMAs, warps 4..7 are the epilogue
+constexpr int kRedPitch = kScaleBlock + 4;
+
+template <int kCols> constexpr int kFewStages = kCols <= 64 ? 4 : 5;
+template <int kCols> constexpr int kFewStageBytes = kOperandBytes + kCols * kScaleBlock;
+template <int kCols> constexpr int kFewSmem = 1024 + kFewStages<kCols> * kFewStageBytes<kCols>;
+static_assert(kFewSmem<16> - 1024 >= 16 * kRedPitch * 4 && kFewSmem<128> - 1024 >= 128 * kRedPitch * 4, "the sums fit the stages");
+
+template <int kType, int kCols>
+__global__ void __launch_bounds__(kFewThreads, kCols <= 64 ? 2 : 1)
+matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
+                  const __grid_constant__ CUtensorMap map_b, int parts) {
+  extern __shared__ unsigned char smem_raw[];
+  constexpr int kS = kFewStages<kCols>;
+  constexpr int kTmem = 2 * kCols < 32 ? 32 : 2 * kCols;
+  __shared__ __align__(8) Wide s_bar[2 * kS + 4];  // full, empty, accumulator full[2] and read out[2]
+  __shared__ __align__(16) float s_scale[4][2][kCols];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int part = static_cast<int>(blockIdx.x) % parts, n0 = static_cast<int>(blockIdx.x) / parts * kScaleBlock;
+  const int m0 = static_cast<int>(blockIdx.y) * kCols;
+  const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * part / parts);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (part + 1) / parts);
+  unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  const uint32_t sbase = smem_addr(smem), bar0 = smem_addr(&s_bar[0]);
+  auto bar_full = [&](int s) { return bar0 + 8u * s; };
+  auto bar_empty = [&](int s) { return bar0 + 8u * (kS + s); };
+  auto bar_acc = [&](int i) { return bar0 + 8u * (2 * kS + i); };
+  auto bar_read = [&](int i) { return bar0 + 8u * (2 * kS + 2 + i); };
+
+  if (tid == 0) {
+    s_fail = 0;
+    for (int s = 0; s < kS; ++s) {
+      bar_init(bar_full(s), 1);
+      bar_init(bar_empty(s), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(bar_acc(i), 1);
+      bar_init(bar_read(i), 4);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(kTmem) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  volatile int* v_fail = &s_fail;
+  auto wait_ok = [&](uint32_t bar, uint32_t parity) {
+    for (int i = 0; i < p.wait_limit; ++i) {
+      if (bar_try_tmem(bar, parity)) return true;
+      if ((i & 63) == 63 && *v_fail) return false;
+    }
+    *v_fail = 1;
+    if (p.status) atomicExch(p.status, KS_ERR_TIMEOUT);
+    return false;
+  };
+
+  float* s_sum = reinterpret_cast<float*>(smem);  // [kCols][kRedPitch], once the stages are done with
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+        const int s = it % kS;
+        if (!wait_ok(bar_empty(s), ((it / kS) & 1u) ^ 1u)) break;
+        bar_expect(bar_full(s), kFewStageBytes<kCols>);
+        if (p.starve) continue;
+        load_one(sbase + s * kFewStageBytes<kCols>, &map_b, kb * kScaleBlock, n0, bar_full(s));
+        load_one(sbase + s * kFewStageBytes<kCols> + kOperandBytes, &map_a, kb * kScaleBlock, m0, bar_full(s));
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = instr_desc(kScaleBlock, kCols);
+      for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+        const int s = it % kS, acc = it & 1;
+        if (!wait_ok(bar_read(acc), ((it >> 1) & 1u) ^ 1u) || !wait_ok(bar_full(s), (it / kS) & 1u)) break;
+        fence_after();
+        const uint64_t dw = operand_desc(sbase + s * kFewStageBytes<kCols>);
+        const uint64_t dx = operand_desc(sbase + s * kFewStageBytes<kCols> + kOperandBytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma<0>(tmem + acc * kCols, dw + 2u * k, dx + 2u * k, idesc, k > 0);
+        commit_one(bar_empty(s));
+        commit_one(bar_acc(acc));
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    const int w = warp - 4;
+    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(w * 32) << 16);
+    constexpr int kLoad = kCols < 32 ? kCols : 32, kEach = (kCols + 31) / 32;
+    Wide sum[kCols / 2];
+#pragma unroll
+    for (int q = 0; q < kCols / 2; ++q) sum[q] = 0;
+    float sa[kEach];
+    const int64_t sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
+    auto fetch = [&](int kb) {
+      const float sb = scale_value(p.b_scale, sb_at + kb, p.scale_type);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int m = m0 + lane + 32 * e;
+        sa[e] = m < p.m && lane + 32 * e < kCols ? scale_value(p.a_scale, static_cast<int64_t>(m) * p.kblocks + kb, p.scale_type) * sb : 0.0f;
+      }
+    };
+    if (kb0 < kb1) fetch(kb0);
+    for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+      const int acc = it & 1;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (lane + 32 * e < kCols) s_scale[w][acc][lane + 32 * e] = sa[e];
+      __syncwarp();
+      if (kb + 1 < kb1) fetch(kb + 1);
+      if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it >> 1) & 1u))) break;
+      fence_after();
+      const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_scale[w][acc]);
+#pragma unroll
+      for (int c = 0; c < kCols; c += kLoad) {
+        uint32_t r[32];
+        if (kCols < 32) {
+          asm volatile(
+              "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+              : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+              : "r"(tmem_mine + acc * kCols));
+#pragma unroll
+          for (int q = 16; q < 32; ++q) r[q] = 0;
+        } else {
+          tmem_ld32(tmem_mine + acc * kCols + c, r);
+        }
+        tmem_wait(r);
+#pragma unroll
+        for (int q = 0; q < kLoad / 4; ++q) {
+          const ulonglong2 f = sc[c / 4 + q];
+          add_scaled(sum[c / 2 + 2 * q], r[4 * q], r[4 * q + 1], f.x);
+          add_scaled(sum[c / 2 + 2 * q + 1], r[4 * q + 2], r[4 * q + 3], f.y);
+        }
+      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_read(acc));
+    }
+    // (the last accumulator is read: every copy has arrived and every MMA is done)
+    asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
+    if (!*v_fail) {
+#pragma unroll
+      for (int q = 0; q < kCols / 2; ++q) {
+        s_sum[(2 * q) * kRedPitch + w * 32 + lane] = low(sum[q]);
+        s_sum[(2 * q + 1) * kRedPitch + w * 32 + lane] = high(sum[q]);
+      }
+    }
+  }
+  if (*v_fail)
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+  __syncthreads();
+  if (parts > 1) cluster_sync();
+  // rows of the result, dealt among the cluster's warps; a warp adds the parts of 128 columns, a lane four neighbours
+  const int rows = p.m - m0 < kCols ? p.m - m0 : kCols;
+  const int n = n0 + 4 * lane;
+  if (!*v_fail)
+    for (int r = part * (kFewThreads / 32) + warp; r < rows; r += parts * (kFewThreads / 32)) {
+      float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      const uint32_t mine = smem_addr(s_sum + r * kRedPitch + 4 * lane);
+      for (int q = 0; q < parts; ++q) {
+        float4 x;
+        const uint32_t from = parts > 1 ? to_cluster(mine, q) : mine;
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(from));
+        v[0] += x.x;
+        v[1] += x.y;
+        v[2] += x.z;
+        v[3] += x.w;
+      }
+      float amax = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = n + e < p.n ? finish(p, v[e], n + e) : 0.0f;
+        amax = fmaxf(amax, finite_abs(v[e]));
+      }
+      const int64_t row = m0 + r;
+      if (kType == KS_E4M3) {
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
+        const float inv = stored_scale(p, amax, row * scale_blocks(p.n) + n0 / kScaleBlock, lane == 0);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= inv;
+      }
+      if (p.wide_rows && n + 4 <= p.n) {
+        char* out = static_cast<char*>(p.d) + (row * p.ldd + n) * kBytes<kType>;
+        if (kType == KS_F32) *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
+        else if (kType == KS_E4M3) *reinterpret_cast<uint32_t*>(out) = pack<kType>(v);
+        else *reinterpret_cast<uint2*>(out) = make_uint2(pack<kType>(v), pack<kType>(v + 2));
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (n + e < p.n) store_one<kType>(p, row * p.ldd + n + e, v[e]);
+      }
+    }
+  if (parts > 1) cluster_sync();  // its sums are read by the others
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
+// host
+// ------------------------------------------------------------------------------------------
+
+// [rows][k] bytes, boxes of `box_rows` rows and 128 of K, in the operands' swizzled form; zeros behind both ends
+cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k, int64_t ld, int box_rows) {
+  std::memset(map, 0, sizeof(*map));
+  if (k == 0) return cudaSuccess;  // (no copy is made)
+  const EncodeTiled fn = encode_tiled();
+  if (!fn) return cudaErrorNotSupported;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(k), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(ld)};
+  const cuuint32_t box[2] = {kScaleBlock, static_cast<cuuint32_t>(box_rows)};
+  const cuuint32_t step[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+template <int kType>
+cudaError_t launch_pair(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
+  // the register split is made for this count
+  static const cudaError_t fits = [] {
+    cudaFuncAttributes attr{};
+    const cudaError_t e = cudaFuncGetAttributes(&attr, reinterpret_cast<const void*>(&matmul_pair_kernel<kType>));
+    return e != cudaSuccess ? e : attr.numRegs == kRegs ? cudaSuccess : cudaErrorInvalidKernelImage;
+  }();
+  if (fits != cudaSuccess) return fits;
+  CUtensorMap ma, mb;
+  cudaError_t e = make_map(&ma, q.a, q.m, q.k, q.lda, kHalf);
+  if (e == cudaSuccess) e = make_map(&mb, q.b, q.n, q.k, q.ldb, kHalf);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void*>(&matmul_pair_kernel<kType>), kSmem);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = ((q.m + kTile - 1) / kTile) * ((q.n + kTile - 1) / kTile);
+  matmul_pair_kernel<kType><<<2 * static_cast<int>(std::min<int64_t>(tiles, kSms / 2)), kThreads, kSmem, stream>>>(p, ma, mb);
+  return cudaGetLastError();
+}
+
+template <int kType, int kCols>
+cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
+  CUtensorMap ma, mb;
+  cudaError_t e = make_map(&ma, q.a, q.m, q.k, q.lda, kCols);
+  if (e == cudaSuccess) e = make_map(&mb, q.b, q.n, q.k, q.ldb, kScaleBlock);
+  const void* kernel = reinterpret_cast<const void*>(&matmul_few_kernel<kType, kCols>);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(kernel, kFewSmem<kCols>);
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = scale_blocks(q.n), rows = (q.m + kCols - 1) / kCols;
+  if (tiles * 8 > INT32_MAX || rows > 65535) return cudaErrorInvalidConfiguration;
+  // parts of K, so that the machine's CTAs have work each
+  int parts = 1;
+  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * (kCols <= 64 ? 2 : 1)) parts *= 2;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows));
+  cfg.blockDim = dim3(kFewThreads);
+  cfg.dynamicSmemBytes = kFewSmem<kCols>;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = static_cast<unsigned>(parts);
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, matmul_few_kernel<kType, kCols>, p, ma, mb, parts);
+}
+
+template <int kType>
+cudaError_t launch_type(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
+  if (q.m <= 16) return launch_few<kType, 16>(q, p, stream);
+  if (q.m <= 32) return launch_few<kType, 32>(q, p, stream);
+  if (q.m <= 64) return launch_few<kType, 64>(q, p, stream);
+  if (q.m <= 128) return launch_few<kType, 128>(q, p, stream);
+  return launch_pair<kType>(q, p, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_matmul_e4m3(const MatmulE4m3& p, int* status, cudaStream_t stream, int64_t* launches, const FastWait* wait) {
-  const int64_t bx = scale_blocks(p.n), by = (p.m + kRows - 1) / kRows;
-  if (by > 65535) return cudaErrorInvalidConfiguration;
-  matmul_kernel<<<dim3(static_cast<unsigned>(bx), static_cast<unsigned>(by)), kThreads, 0, stream>>>(p);
+cudaError_t launch_matmul_e4m3(const MatmulE4m3& q, int* status, cudaStream_t stream, int64_t* launches, const FastWait* wait) {
+  const int bytes = q.d_type == KS_F32 ? 4 : q.d_type == KS_E4M3 ? 1 : 2;
+  MatmulArgs p{};
+  p.a_scale = q.a_scale;
+  p.b_scale = q.b_scale;
+  p.scale_type = q.scale_type;
+  p.m = static_cast<int>(q.m);
+  p.n = static_cast<int>(q.n);
+  p.kblocks = static_cast<int>(scale_blocks(q.k));
+  p.bias = q.bias;
+  p.relu = q.relu;
+  p.d = q.d;
+  p.ldd = q.ldd;
+  p.wide_rows = reinterpret_cast<uintptr_t>(q.d) % 32 == 0 && (q.m == 1 || q.ldd * bytes % 32 == 0);
+  p.d_scale = q.d_scale;
+  p.wait_limit = wait->limit > 0 ? wait->limit : kMlpWaitLimit;
+  p.starve = wait->starve;
+  p.status = status;
   ++*launches;
-  return cudaGetLastError();
+  switch (q.d_type) {
+    case KS_F32: return launch_type<KS_F32>(q, p, stream);
+    case KS_BF16: return launch_type<KS_BF16>(q, p, stream);
+    case KS_F16: return launch_type<KS_F16>(q, p, stream);
+    default: return launch_type<KS_E4M3>(q, p, stream);
+  }
 }
 
 }  // namespace ks
