@@ -49,11 +49,15 @@ __device__ __forceinline__ float e8m0_value(uint32_t b) {  // (0 is 2^-127, belo
   return b == 0u ? __uint_as_float(0x400000u) : b == 255u ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float(b << 23);
 }
 
-// Two scaled values as e4m3, `lo` in the low byte; what is not finite becomes the code that is no number.
-__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+// Two scaled values as e4m3, `lo` in the low byte; what is not finite becomes the code that is no number. The first form is for
+// values that are not infinite (the conversion makes 448 of those).
+__device__ __forceinline__ uint32_t e4m3_pair_finite(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  uint32_t v = r;
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3_pair(float lo, float hi) {
+  uint32_t v = e4m3_pair_finite(lo, hi);
   const float inf = __int_as_float(0x7F800000);
   if (fabsf(lo) == inf) v |= 0x7Fu;
   if (fabsf(hi) == inf) v |= 0x7F00u;

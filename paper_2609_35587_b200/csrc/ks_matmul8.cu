@@ -134,15 +134,24 @@ __device__ __forceinline__ float stored_scale(const MatmulArgs& p, float amax, i
 // many rows: pairs of CTAs, 256 x 256 of the result at a time
 // ------------------------------------------------------------------------------------------
 
-constexpr int kThreads = 384;  // warp 0 loads, warp 1 issues MMAs, warps 4..11 are the epilogue
+// Two warps that have nothing else to do bring the scales, eight blocks of K at a time: the epilogue's threads would each read
+// a row's, 32 sectors an instruction, which cost a fifth of the kernel's time.
+constexpr int kThreads = 384;  // warp 0 loads, warp 1 issues MMAs, warps 2 and 3 bring scales, warps 4..11 are the epilogue
 constexpr int kRegs = 168, kRegsFew = 56, kRegsEpilogue = 224;  // a thread's registers at launch, and after the split
 static_assert(128 * kRegsFew + 256 * kRegsEpilogue <= kThreads * kRegs, "the split hands out what the block was launched with");
 constexpr int kTile = 256, kHalf = kTile / 2;
 constexpr int kStages = 6;
 constexpr int kOperandBytes = kHalf * kScaleBlock;  // a CTA's 128 rows of A, or its half of B's
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kStoreFloats = 32 * 33;  // of a warp, for results whose rows do not begin on 32-byte boundaries
-constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStoreFloats * 4;
+constexpr int kChunk = 8;  // blocks of K whose scales are brought together
+constexpr int kStorePitch = 17;
+struct PairShared {  // behind the stages
+  float a_scale[2][kChunk][kHalf];
+  float b_scale[2][2][kChunk];
+  float bias[2][kTile];
+  float store[8][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 32-byte boundaries
+};
+constexpr int kSmem = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(PairShared));
 constexpr int kGroup = 8;  // row tiles that share a stretch of column tiles, for L2
 
 struct Tile {
@@ -156,13 +165,92 @@ __device__ __forceinline__ Tile tile_at(int64_t t, int tiles_m, int tiles_n) {
   return Tile{(first + in % rows) * kTile, (in / rows) * kTile};
 }
 
+// A thread's 128 neighbouring elements of a row, written as they are rounded to.
+template <int kType>
+__device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, Wide (&sum)[kHalf / 2], const float* bias, float* s_store) {
+  const int lane = threadIdx.x & 31;
+  if (p.bias) {
+    const ulonglong2* b = reinterpret_cast<const ulonglong2*>(bias);
+#pragma unroll
+    for (int q = 0; q < kHalf / 4; ++q) {
+      const ulonglong2 x = b[q];
+      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q]) : "l"(x.x));
+      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q + 1]) : "l"(x.y));
+    }
+  }
+  if (p.relu) {
+#pragma unroll
+    for (int q = 0; q < kHalf / 2; ++q)  // (of what is not a number 0)
+      sum[q] = (static_cast<Wide>(__float_as_uint(fmaxf(high(sum[q]), 0.0f))) << 32) | __float_as_uint(fmaxf(low(sum[q]), 0.0f));
+  }
+  float inv = 1.0f;
+  bool odd = false;  // of the values some may be infinite
+  if (kType == KS_E4M3) {
+    float amax = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kHalf / 2; ++q) amax = fmaxf(amax, fmaxf(fabsf(low(sum[q])), fabsf(high(sum[q]))));
+    odd = amax == __int_as_float(0x7F800000);
+    if (odd) {
+      amax = 0.0f;
+#pragma unroll
+      for (int q = 0; q < kHalf / 2; ++q) amax = fmaxf(amax, fmaxf(finite_abs(low(sum[q])), finite_abs(high(sum[q]))));
+    }
+    inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock, row < p.m);
+    const Wide inv2 = both(inv);
+#pragma unroll
+    for (int q = 0; q < kHalf / 2; ++q) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(sum[q]) : "l"(inv2));
+  }
+  constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
+  if (p.wide_rows && n0 + kHalf <= p.n) {
+    char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row) * p.ldd + n0) * kBytes<kType>;
+#pragma unroll
+    for (int g = 0; g < kHalf / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int c = (g * 8 + i) * kPer;
+        if (kType == KS_E4M3) {
+          const float v[4] = {low(sum[c / 2]), high(sum[c / 2]), low(sum[c / 2 + 1 < kHalf / 2 ? c / 2 + 1 : 0]),
+                              high(sum[c / 2 + 1 < kHalf / 2 ? c / 2 + 1 : 0])};
+          w[i] = odd ? e4m3_quad(v[0], v[1], v[2], v[3]) : e4m3_pair_finite(v[0], v[1]) | (e4m3_pair_finite(v[2], v[3]) << 16);
+        } else {
+          const float v[2] = {c & 1 ? high(sum[c / 2]) : low(sum[c / 2]), high(sum[c / 2])};
+          w[i] = pack<kType>(v);
+        }
+      }
+      if (row < p.m)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 32 * g), "r"(w[0]), "r"(w[1]),
+                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    }
+    return;
+  }
+  // through shared memory, so that neighbouring threads write neighbouring elements of a row: 16 columns at a time
+#pragma unroll
+  for (int c0 = 0; c0 < kHalf; c0 += 16) {
+    if (n0 + c0 >= p.n) break;
+    __syncwarp();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      s_store[lane * kStorePitch + 2 * q] = low(sum[c0 / 2 + q]);
+      s_store[lane * kStorePitch + 2 * q + 1] = high(sum[c0 / 2 + q]);
+    }
+    __syncwarp();
+    const int n = n0 + c0 + lane % 16, row0 = row - lane;
+    if (n < p.n)
+      for (int r = lane / 16; r < 32 && row0 + r < p.m; r += 2)
+        store_one<kType>(p, static_cast<int64_t>(row0 + r) * p.ldd + n, s_store[r * kStorePitch + lane % 16]);
+  }
+}
+
 template <int kType>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
                    const __grid_constant__ CUtensorMap map_b) {
   extern __shared__ unsigned char smem_raw[];
-  // full[kStages] (the leader's are used), empty[kStages], accumulator full[2] and read out[2] (the leader's)
-  __shared__ __align__(8) Wide s_bar[2 * kStages + 4];
+  // full[kStages] (the leader's are used), empty[kStages], accumulator full[2] and read out[2] (the leader's), scales full[2]
+  // and used[2]
+  __shared__ __align__(8) Wide s_bar[2 * kStages + 8];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
@@ -170,11 +258,14 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   const uint32_t rank = blockIdx.x & 1;  // CTA of the pair; 0 issues the MMAs
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
   unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  PairShared& sh = *reinterpret_cast<PairShared*>(smem + kStages * kStageBytes);
   const uint32_t sbase = smem_addr(smem), bar0 = smem_addr(&s_bar[0]);
   auto bar_full = [&](int s) { return bar0 + 8u * s; };
   auto bar_empty = [&](int s) { return bar0 + 8u * (kStages + s); };
-  auto bar_acc = [&](int i) { return bar0 + 8u * (2 * kStages + i); };
-  auto bar_read = [&](int i) { return bar0 + 8u * (2 * kStages + 2 + i); };
+  auto bar_acc = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + i); };
+  auto bar_read = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 2 + i); };
+  auto bar_scale = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 4 + i); };
+  auto bar_used = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 6 + i); };
 
   if (tid == 0) {
     s_fail = 0;
@@ -185,6 +276,8 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     for (int i = 0; i < 2; ++i) {
       bar_init(bar_acc(i), 1);
       bar_init(bar_read(i), 16);  // eight epilogue warps of each CTA
+      bar_init(bar_scale(i), 2);
+      bar_init(bar_used(i), 8);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -199,11 +292,13 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   const uint32_t tmem = s_tmem;
   const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
   const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
+  const int chunks = p.kblocks > 0 ? (p.kblocks + kChunk - 1) / kChunk : 1;
   volatile int* v_fail = &s_fail;
 
   // Bounded wait; after the first that runs out every role of the CTA leaves its loop, and the pair's other CTA runs into
   // its own limit.
   auto wait_ok = [&](uint32_t bar, uint32_t parity) {
+    if (bar_try_tmem(bar, parity)) return true;
     for (int i = 0; i < p.wait_limit; ++i) {
       if (bar_try_tmem(bar, parity)) return true;
       if ((i & 63) == 63 && *v_fail) return false;
@@ -215,155 +310,153 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    // The warps that load and issue stay together and one lane of them does the work, so that what it works with is uniform:
+    // a lane of its own took 250 clocks for a wait that was over and as many for four MMAs.
     if (warp == 0) {
-      if (lane == 0) {
-        uint32_t it = 0;
-        bool ok = true;
-        for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
-          const Tile at = tile_at(t, tiles_m, tiles_n);
-          for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-            const int s = static_cast<int>(it % kStages);
-            if (!(ok = wait_ok(bar_empty(s), ((it / kStages) & 1u) ^ 1u))) break;
-            const uint32_t full = to_cluster(bar_full(s), 0), dst = sbase + s * kStageBytes;
+      const bool lead = elect_one();
+      uint32_t s = 0, parity = 1;
+      bool ok = true;
+      for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+        const Tile at = tile_at(t, tiles_m, tiles_n);
+        const int row_a = at.m + static_cast<int>(rank) * kHalf, row_b = at.n + static_cast<int>(rank) * kHalf;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!(ok = wait_ok(bar_empty(s), parity))) break;
+          const uint32_t full = to_cluster(bar_full(s), 0), dst = sbase + s * kStageBytes;
+          if (lead) {
             if (rank == 0) bar_expect(bar_full(s), 2u * kStageBytes);
-            if (p.starve) continue;  // test hook: without the copies the waits on this barrier run out
-            load_pair(dst, &map_a, kb * kScaleBlock, at.m + static_cast<int>(rank) * kHalf, full);
-            load_pair(dst + kOperandBytes, &map_b, kb * kScaleBlock, at.n + static_cast<int>(rank) * kHalf, full);
+            if (!p.starve) {  // test hook: without the copies the waits on this barrier run out
+              load_pair(dst, &map_a, kb * kScaleBlock, row_a, full);
+              load_pair(dst + kOperandBytes, &map_b, kb * kScaleBlock, row_b, full);
+            }
+          }
+          if (++s == kStages) {
+            s = 0;
+            parity ^= 1u;
           }
         }
       }
       __syncwarp();
     } else if (warp == 1) {
-      if (rank == 0 && lane == 0) {
-        uint32_t it = 0;
+      if (rank == 0) {
+        const bool lead = elect_one();
+        uint32_t s = 0, parity = 0, acc = 0, parity_acc = 1;
         bool ok = true;
         constexpr uint32_t idesc = instr_desc(kTile, kTile);
+        const uint64_t desc0 = operand_desc(sbase);
         for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
-          for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-            const uint32_t acc = it & 1u;
-            const int s = static_cast<int>(it % kStages);
-            if (!(ok = wait_ok(bar_read(acc), ((it >> 1) & 1u) ^ 1u) && wait_ok(bar_full(s), (it / kStages) & 1u))) break;
+          for (int kb = 0; kb < p.kblocks; ++kb) {
+            if (!(ok = wait_ok(bar_read(acc), parity_acc) && wait_ok(bar_full(s), parity))) break;
             fence_after();
-            const uint64_t da = operand_desc(sbase + s * kStageBytes), db = operand_desc(sbase + s * kStageBytes + kOperandBytes);
+            const uint64_t da = desc0 + s * (kStageBytes >> 4), db = da + (kOperandBytes >> 4);
+            const uint32_t d = tmem + acc * kTile;
+            if (lead) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
-              mma<1>(tmem + acc * kTile, da + 2u * k, db + 2u * k, idesc, k > 0);
-            commit_pair(bar_empty(s));
-            commit_pair(bar_acc(acc));
+              for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
+                mma<1>(d, da + 2u * k, db + 2u * k, idesc, k > 0);
+              commit_pair(bar_empty(s));
+              commit_pair(bar_acc(acc));
+            }
+            if (++s == kStages) {
+              s = 0;
+              parity ^= 1u;
+            }
+            acc ^= 1u;
+            if (acc == 0) parity_acc ^= 1u;
           }
         }
       }
       __syncwarp();
+    } else {
+      // scales of this CTA's rows and of both blocks of columns; with a tile's first also its bias
+      const int r0 = (warp - 2) * 64 + lane;
+      uint32_t it = 0;
+      bool ok = true;
+      uint32_t tile_par = 0;
+      for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
+        const Tile at = tile_at(t, tiles_m, tiles_n);
+        for (int c = 0; c < chunks; ++c, ++it) {
+          const uint32_t buf = it & 1u;
+          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_used(buf), ((it >> 1) & 1u) ^ 1u)))) break;
+          const int kb0 = c * kChunk, n_kb = p.kblocks - kb0 < kChunk ? p.kblocks - kb0 : kChunk;
+          if (c == 0 && p.bias)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int n = (warp - 2) * kHalf + 32 * i + lane;
+              sh.bias[tile_par][n] = at.n + n < p.n ? __ldg(p.bias + at.n + n) : 0.0f;
+            }
+          float v[2][kChunk], w = 0.0f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = at.m + static_cast<int>(rank) * kHalf + r0 + 32 * h;
+            const int64_t from = static_cast<int64_t>(row < p.m ? row : 0) * p.kblocks + kb0;
+#pragma unroll
+            for (int k = 0; k < kChunk; ++k) v[h][k] = k < n_kb ? scale_value(p.a_scale, from + k, p.scale_type) : 0.0f;
+          }
+          const int j = warp - 2, nb = at.n / kScaleBlock + j;
+          if (lane < n_kb && nb * kScaleBlock < p.n) w = scale_value(p.b_scale, static_cast<int64_t>(nb) * p.kblocks + kb0 + lane, p.scale_type);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < kChunk; ++k) sh.a_scale[buf][k][r0 + 32 * h] = v[h][k];
+          if (lane < kChunk) sh.b_scale[buf][j][lane] = w;
+          __syncwarp();
+          if (lane == 0) bar_arrive(bar_scale(buf));
+        }
+      }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
-    // warp w owns lanes 32 (w % 4) .. and one half of a tile's columns: 128, a block of the result's and of the weights' scales
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
+    // warp w owns lanes 32 (w % 4) .. and one block of a tile's columns
+    const int quarter = warp & 3, j = (warp - 4) >> 2;
     const int trow = quarter * 32 + lane;
-    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + half * kHalf;
-    float* s_store = reinterpret_cast<float*>(smem + kStages * kStageBytes) + (warp - 4) * kStoreFloats;
-    uint32_t it = 0;
+    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j * kHalf;
+    uint32_t used = 0, it = 0, tile_par = 0;
     bool ok = true;
-    for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+    for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
       const Tile at = tile_at(t, tiles_m, tiles_n);
-      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + half * kHalf;
+      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + j * kHalf;
       const bool inside = n0 < p.n;  // (of the warp's columns any)
-      const int64_t sa_at = static_cast<int64_t>(row < p.m ? row : p.m - 1) * p.kblocks;
-      const int64_t sb_at = static_cast<int64_t>(inside ? n0 / kScaleBlock : 0) * p.kblocks;
       Wide sum[kHalf / 2];
 #pragma unroll
       for (int q = 0; q < kHalf / 2; ++q) sum[q] = 0;
-      float sa = 0.0f, sb = 0.0f;
-      if (p.kblocks > 0) {
-        sa = scale_value(p.a_scale, sa_at, p.scale_type);
-        sb = scale_value(p.b_scale, sb_at, p.scale_type);
-      }
-      for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-        const uint32_t acc = it & 1u;
-        const Wide s = both(sa * sb);
-        if (kb + 1 < p.kblocks) {  // on their way while the accumulator is waited for
-          sa = scale_value(p.a_scale, sa_at + kb + 1, p.scale_type);
-          sb = scale_value(p.b_scale, sb_at + kb + 1, p.scale_type);
-        }
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it >> 1) & 1u)))) break;
-        fence_after();
-        if (inside) {
+      for (int c = 0; c < chunks && ok; ++c, ++it) {
+        const uint32_t buf = it & 1u;
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_scale(buf), (it >> 1) & 1u)))) break;
+        const int n_kb = p.kblocks - c * kChunk < kChunk ? p.kblocks - c * kChunk : kChunk;
+        for (int k = 0; k < n_kb; ++k, ++used) {
+          const uint32_t acc = used & 1u;
+          const Wide s = both(sh.a_scale[buf][k][trow] * sh.b_scale[buf][j][k]);
+          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (used >> 1) & 1u)))) break;
+          fence_after();
+          if (!inside) {
+            fence_before();
+            if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
+            continue;
+          }
           uint32_t r[2][32];
           tmem_ld32(tmem_mine + acc * kTile, r[0]);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tmem_wait(r[c & 1]);
-            if (c < 3) {
-              tmem_ld32(tmem_mine + acc * kTile + 32 * (c + 1), r[(c + 1) & 1]);
+          for (int q0 = 0; q0 < 4; ++q0) {
+            tmem_wait(r[q0 & 1]);
+            if (q0 < 3) {
+              tmem_ld32(tmem_mine + acc * kTile + 32 * (q0 + 1), r[(q0 + 1) & 1]);
             } else {
               fence_before();
               if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
             }
 #pragma unroll
-            for (int q = 0; q < 16; ++q) add_scaled(sum[16 * c + q], r[c & 1][2 * q], r[c & 1][2 * q + 1], s);
+            for (int q = 0; q < 16; ++q) add_scaled(sum[16 * q0 + q], r[q0 & 1][2 * q], r[q0 & 1][2 * q + 1], s);
           }
-        } else {
-          fence_before();
-          if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
         }
-      }
-      if (!ok || !inside) continue;
-      float inv = 1.0f;
-      if (kType == KS_E4M3) {
-        float amax = 0.0f;
-#pragma unroll
-        for (int q = 0; q < kHalf / 2; ++q) {
-          const int n = n0 + 2 * q;
-          float lo = 0.0f, hi = 0.0f;
-          if (n < p.n) lo = finish(p, low(sum[q]), n);
-          if (n + 1 < p.n) hi = finish(p, high(sum[q]), n + 1);
-          amax = fmaxf(amax, fmaxf(finite_abs(lo), finite_abs(hi)));
-          sum[q] = (static_cast<Wide>(__float_as_uint(hi)) << 32) | __float_as_uint(lo);
-        }
-        inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock, row < p.m);
-      }
-      constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
-      if (p.wide_rows && n0 + kHalf <= p.n) {
-        char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row) * p.ldd + n0) * kBytes<kType>;
-#pragma unroll
-        for (int g = 0; g < kHalf / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
-          uint32_t w[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) {
-              const int c = (g * 8 + i) * kPer + e;
-              const float x = c & 1 ? high(sum[c / 2]) : low(sum[c / 2]);
-              v[e] = kType == KS_E4M3 ? x * inv : finish(p, x, n0 + c);
-            }
-            w[i] = pack<kType>(v);
-          }
-          if (row < p.m)
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 32 * g), "r"(w[0]), "r"(w[1]),
-                         "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-                         : "memory");
-        }
-      } else {
-        // through shared memory, so that neighbouring threads write neighbouring elements of a row
-#pragma unroll
-        for (int c0 = 0; c0 < kHalf; c0 += 32) {
-          if (n0 + c0 >= p.n) break;
+        if (ok && c + 1 < chunks) {
           __syncwarp();
-#pragma unroll
-          for (int q = 0; q < 16; ++q) {
-            s_store[lane * 33 + 2 * q] = low(sum[c0 / 2 + q]) * inv;
-            s_store[lane * 33 + 2 * q + 1] = high(sum[c0 / 2 + q]) * inv;
-          }
-          __syncwarp();
-          const int n = n0 + c0 + lane, row0 = row - lane;
-          if (n < p.n)
-            for (int r = 0; r < 32 && row0 + r < p.m; ++r) {
-              const float x = s_store[r * 33 + lane];
-              store_one<kType>(p, static_cast<int64_t>(row0 + r) * p.ldd + n, kType == KS_E4M3 ? x : finish(p, x, n));
-            }
+          if (lane == 0) bar_arrive(bar_used(buf));
         }
       }
+      if (!ok) break;
+      if (inside) store_block<kType>(p, row, n0, sum, sh.bias[tile_par] + j * kHalf, sh.store[warp - 4]);
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_used((it - 1) & 1u));  // (with the last chunk's scales the bias is read too)
     }
   }
   // after a failure: time for the copies and MMAs in flight to end
