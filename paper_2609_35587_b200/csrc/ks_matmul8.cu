@@ -135,21 +135,24 @@ __device__ __forceinline__ float stored_scale(const MatmulArgs& p, float amax, i
 // ------------------------------------------------------------------------------------------
 
 // Two warps that have nothing else to do bring the scales, eight blocks of K at a time: the epilogue's threads would each read
-// a row's, 32 sectors an instruction, which cost a fifth of the kernel's time.
-constexpr int kThreads = 384;  // warp 0 loads, warp 1 issues MMAs, warps 2 and 3 bring scales, warps 4..11 are the epilogue
-constexpr int kRegs = 168, kRegsFew = 56, kRegsEpilogue = 224;  // a thread's registers at launch, and after the split
-static_assert(128 * kRegsFew + 256 * kRegsEpilogue <= kThreads * kRegs, "the split hands out what the block was launched with");
+// a row's, 32 sectors an instruction, which cost a fifth of the kernel's time. The epilogue has sixteen warps of 64 columns:
+// what a warp does for a block of K is a chain of waits and loads, and four warps a scheduler hide each other's.
+constexpr int kThreads = 640;  // warp 0 loads, warp 1 issues MMAs, warps 2 and 3 bring scales, warps 4..19 are the epilogue
+constexpr int kRegs = 96, kRegsFew = 32, kRegsEpilogue = 112;  // a thread's registers at launch, and after the split
+static_assert(128 * kRegsFew + 512 * kRegsEpilogue <= kThreads * kRegs, "the split hands out what the block was launched with");
 constexpr int kTile = 256, kHalf = kTile / 2;
 constexpr int kStages = 6;
 constexpr int kOperandBytes = kHalf * kScaleBlock;  // a CTA's 128 rows of A, or its half of B's
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kChunk = 8;  // blocks of K whose scales are brought together
-constexpr int kStorePitch = 17;
+constexpr int kCols = 64;  // of an epilogue warp
+constexpr int kStorePitch = 9;
 struct PairShared {  // behind the stages
   float a_scale[2][kChunk][kHalf];
   float b_scale[2][2][kChunk];
   float bias[2][kTile];
-  float store[8][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 32-byte boundaries
+  float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 32-byte boundaries
+  float amax[2][16][32];  // of a warp's rows, for the one that has the block's other half
 };
 constexpr int kSmem = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(PairShared));
 constexpr int kGroup = 8;  // row tiles that share a stretch of column tiles, for L2
@@ -165,14 +168,12 @@ __device__ __forceinline__ Tile tile_at(int64_t t, int tiles_m, int tiles_n) {
   return Tile{(first + in % rows) * kTile, (in / rows) * kTile};
 }
 
-// A thread's 128 neighbouring elements of a row, written as they are rounded to.
-template <int kType>
-__device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, Wide (&sum)[kHalf / 2], const float* bias, float* s_store) {
-  const int lane = threadIdx.x & 31;
+// Bias and ReLU on a thread's 64 neighbouring elements of a row.
+__device__ __forceinline__ void finish_block(const MatmulArgs& p, Wide (&sum)[kCols / 2], const float* bias) {
   if (p.bias) {
     const ulonglong2* b = reinterpret_cast<const ulonglong2*>(bias);
 #pragma unroll
-    for (int q = 0; q < kHalf / 4; ++q) {
+    for (int q = 0; q < kCols / 4; ++q) {
       const ulonglong2 x = b[q];
       asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q]) : "l"(x.x));
       asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q + 1]) : "l"(x.y));
@@ -180,39 +181,41 @@ __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0
   }
   if (p.relu) {
 #pragma unroll
-    for (int q = 0; q < kHalf / 2; ++q)  // (of what is not a number 0)
+    for (int q = 0; q < kCols / 2; ++q)  // (of what is not a number 0)
       sum[q] = (static_cast<Wide>(__float_as_uint(fmaxf(high(sum[q]), 0.0f))) << 32) | __float_as_uint(fmaxf(low(sum[q]), 0.0f));
   }
-  float inv = 1.0f;
-  bool odd = false;  // of the values some may be infinite
-  if (kType == KS_E4M3) {
-    float amax = 0.0f;
+}
+
+// Largest magnitude of them; `odd`: some may be infinite (those do not count).
+__device__ __forceinline__ float block_max(const Wide (&sum)[kCols / 2], bool& odd) {
+  float amax = 0.0f;
 #pragma unroll
-    for (int q = 0; q < kHalf / 2; ++q) amax = fmaxf(amax, fmaxf(fabsf(low(sum[q])), fabsf(high(sum[q]))));
-    odd = amax == __int_as_float(0x7F800000);
-    if (odd) {
-      amax = 0.0f;
+  for (int q = 0; q < kCols / 2; ++q) amax = fmaxf(amax, fmaxf(fabsf(low(sum[q])), fabsf(high(sum[q]))));
+  odd = amax == __int_as_float(0x7F800000);
+  if (odd) {
+    amax = 0.0f;
 #pragma unroll
-      for (int q = 0; q < kHalf / 2; ++q) amax = fmaxf(amax, fmaxf(finite_abs(low(sum[q])), finite_abs(high(sum[q]))));
-    }
-    inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock, row < p.m);
-    const Wide inv2 = both(inv);
-#pragma unroll
-    for (int q = 0; q < kHalf / 2; ++q) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(sum[q]) : "l"(inv2));
+    for (int q = 0; q < kCols / 2; ++q) amax = fmaxf(amax, fmaxf(finite_abs(low(sum[q])), finite_abs(high(sum[q]))));
   }
+  return amax;
+}
+
+// Writes them, rounded to the result's type (e4m3: already scaled).
+template <int kType>
+__device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, const Wide (&sum)[kCols / 2], bool odd, float* s_store) {
+  const int lane = threadIdx.x & 31;
   constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
-  if (p.wide_rows && n0 + kHalf <= p.n) {
+  if (p.wide_rows && n0 + kCols <= p.n) {
     char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row) * p.ldd + n0) * kBytes<kType>;
 #pragma unroll
-    for (int g = 0; g < kHalf / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
+    for (int g = 0; g < kCols / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
       uint32_t w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int c = (g * 8 + i) * kPer;
         if (kType == KS_E4M3) {
-          const float v[4] = {low(sum[c / 2]), high(sum[c / 2]), low(sum[c / 2 + 1 < kHalf / 2 ? c / 2 + 1 : 0]),
-                              high(sum[c / 2 + 1 < kHalf / 2 ? c / 2 + 1 : 0])};
-          w[i] = odd ? e4m3_quad(v[0], v[1], v[2], v[3]) : e4m3_pair_finite(v[0], v[1]) | (e4m3_pair_finite(v[2], v[3]) << 16);
+          const Wide x = sum[c / 2], y = sum[c / 2 + 1 < kCols / 2 ? c / 2 + 1 : 0];
+          w[i] = odd ? e4m3_quad(low(x), high(x), low(y), high(y)) : e4m3_pair_finite(low(x), high(x)) | (e4m3_pair_finite(low(y), high(y)) << 16);
         } else {
           const float v[2] = {c & 1 ? high(sum[c / 2]) : low(sum[c / 2]), high(sum[c / 2])};
           w[i] = pack<kType>(v);
@@ -225,21 +228,21 @@ __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0
     }
     return;
   }
-  // through shared memory, so that neighbouring threads write neighbouring elements of a row: 16 columns at a time
+  // through shared memory, so that neighbouring threads write neighbouring elements of a row: 8 columns at a time
 #pragma unroll
-  for (int c0 = 0; c0 < kHalf; c0 += 16) {
+  for (int c0 = 0; c0 < kCols; c0 += 8) {
     if (n0 + c0 >= p.n) break;
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
+    for (int q = 0; q < 4; ++q) {
       s_store[lane * kStorePitch + 2 * q] = low(sum[c0 / 2 + q]);
       s_store[lane * kStorePitch + 2 * q + 1] = high(sum[c0 / 2 + q]);
     }
     __syncwarp();
-    const int n = n0 + c0 + lane % 16, row0 = row - lane;
+    const int n = n0 + c0 + lane % 8, row0 = row - lane;
     if (n < p.n)
-      for (int r = lane / 16; r < 32 && row0 + r < p.m; r += 2)
-        store_one<kType>(p, static_cast<int64_t>(row0 + r) * p.ldd + n, s_store[r * kStorePitch + lane % 16]);
+      for (int r = lane / 8; r < 32 && row0 + r < p.m; r += 4)
+        store_one<kType>(p, static_cast<int64_t>(row0 + r) * p.ldd + n, s_store[r * kStorePitch + lane % 8]);
   }
 }
 
@@ -249,8 +252,8 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
                    const __grid_constant__ CUtensorMap map_b) {
   extern __shared__ unsigned char smem_raw[];
   // full[kStages] (the leader's are used), empty[kStages], accumulator full[2] and read out[2] (the leader's), scales full[2]
-  // and used[2]
-  __shared__ __align__(8) Wide s_bar[2 * kStages + 8];
+  // and used[2], halves of a block's maxima [8]
+  __shared__ __align__(8) Wide s_bar[2 * kStages + 16];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
@@ -266,6 +269,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   auto bar_read = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 2 + i); };
   auto bar_scale = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 4 + i); };
   auto bar_used = [&](uint32_t i) { return bar0 + 8u * (2 * kStages + 6 + i); };
+  auto bar_max = [&](int i) { return bar0 + 8u * (2 * kStages + 8 + i); };
 
   if (tid == 0) {
     s_fail = 0;
@@ -275,10 +279,11 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(bar_acc(i), 1);
-      bar_init(bar_read(i), 16);  // eight epilogue warps of each CTA
+      bar_init(bar_read(i), 32);  // sixteen epilogue warps of each CTA
       bar_init(bar_scale(i), 2);
-      bar_init(bar_used(i), 8);
+      bar_init(bar_used(i), 16);
     }
+    for (int i = 0; i < 8; ++i) bar_init(bar_max(i), 2);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 2) {
@@ -384,20 +389,19 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
               const int n = (warp - 2) * kHalf + 32 * i + lane;
               sh.bias[tile_par][n] = at.n + n < p.n ? __ldg(p.bias + at.n + n) : 0.0f;
             }
-          float v[2][kChunk], w = 0.0f;
-#pragma unroll
+          const int j = warp - 2, nb = at.n / kScaleBlock + j;
+          float w = 0.0f;
+          if (lane < n_kb && nb * kScaleBlock < p.n) w = scale_value(p.b_scale, static_cast<int64_t>(nb) * p.kblocks + kb0 + lane, p.scale_type);
+#pragma unroll 1
           for (int h = 0; h < 2; ++h) {
             const int row = at.m + static_cast<int>(rank) * kHalf + r0 + 32 * h;
             const int64_t from = static_cast<int64_t>(row < p.m ? row : 0) * p.kblocks + kb0;
+            float v[kChunk];
 #pragma unroll
-            for (int k = 0; k < kChunk; ++k) v[h][k] = k < n_kb ? scale_value(p.a_scale, from + k, p.scale_type) : 0.0f;
+            for (int k = 0; k < kChunk; ++k) v[k] = k < n_kb ? scale_value(p.a_scale, from + k, p.scale_type) : 0.0f;
+#pragma unroll
+            for (int k = 0; k < kChunk; ++k) sh.a_scale[buf][k][r0 + 32 * h] = v[k];
           }
-          const int j = warp - 2, nb = at.n / kScaleBlock + j;
-          if (lane < n_kb && nb * kScaleBlock < p.n) w = scale_value(p.b_scale, static_cast<int64_t>(nb) * p.kblocks + kb0 + lane, p.scale_type);
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int k = 0; k < kChunk; ++k) sh.a_scale[buf][k][r0 + 32 * h] = v[h][k];
           if (lane < kChunk) sh.b_scale[buf][j][lane] = w;
           __syncwarp();
           if (lane == 0) bar_arrive(bar_scale(buf));
@@ -406,19 +410,20 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
-    // warp w owns lanes 32 (w % 4) .. and one block of a tile's columns
-    const int quarter = warp & 3, j = (warp - 4) >> 2;
+    // warp w owns lanes 32 (w % 4) .. and 64 of a tile's columns, half of block j
+    const int quarter = warp & 3, part = (warp - 4) >> 2, j = part >> 1;
     const int trow = quarter * 32 + lane;
-    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + j * kHalf;
+    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
+    const uint32_t read0 = to_cluster(bar_read(0), 0);
     uint32_t used = 0, it = 0, tile_par = 0;
     bool ok = true;
     for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
       const Tile at = tile_at(t, tiles_m, tiles_n);
-      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + j * kHalf;
+      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + part * kCols;
       const bool inside = n0 < p.n;  // (of the warp's columns any)
-      Wide sum[kHalf / 2];
+      Wide sum[kCols / 2];
 #pragma unroll
-      for (int q = 0; q < kHalf / 2; ++q) sum[q] = 0;
+      for (int q = 0; q < kCols / 2; ++q) sum[q] = 0;
       for (int c = 0; c < chunks && ok; ++c, ++it) {
         const uint32_t buf = it & 1u;
         if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_scale(buf), (it >> 1) & 1u)))) break;
@@ -428,24 +433,20 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
           const Wide s = both(sh.a_scale[buf][k][trow] * sh.b_scale[buf][j][k]);
           if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (used >> 1) & 1u)))) break;
           fence_after();
-          if (!inside) {
-            fence_before();
-            if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
-            continue;
+          uint32_t r[32];
+          if (inside) {
+            tmem_ld32(tmem_mine + acc * kTile, r);
+            tmem_wait(r);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) add_scaled(sum[q], r[2 * q], r[2 * q + 1], s);
+            tmem_ld32(tmem_mine + acc * kTile + 32, r);
+            tmem_wait(r);
           }
-          uint32_t r[2][32];
-          tmem_ld32(tmem_mine + acc * kTile, r[0]);
+          fence_before();
+          if (lane == 0) bar_arrive_tmem(read0 + 8u * acc);
+          if (inside) {
 #pragma unroll
-          for (int q0 = 0; q0 < 4; ++q0) {
-            tmem_wait(r[q0 & 1]);
-            if (q0 < 3) {
-              tmem_ld32(tmem_mine + acc * kTile + 32 * (q0 + 1), r[(q0 + 1) & 1]);
-            } else {
-              fence_before();
-              if (lane == 0) bar_arrive_tmem(to_cluster(bar_read(acc), 0));
-            }
-#pragma unroll
-            for (int q = 0; q < 16; ++q) add_scaled(sum[16 * q0 + q], r[q0 & 1][2 * q], r[q0 & 1][2 * q + 1], s);
+            for (int q = 0; q < 16; ++q) add_scaled(sum[16 + q], r[2 * q], r[2 * q + 1], s);
           }
         }
         if (ok && c + 1 < chunks) {
@@ -454,7 +455,23 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
         }
       }
       if (!ok) break;
-      if (inside) store_block<kType>(p, row, n0, sum, sh.bias[tile_par] + j * kHalf, sh.store[warp - 4]);
+      finish_block(p, sum, sh.bias[tile_par] + part * kCols);
+      bool odd = false;
+      if (kType == KS_E4M3) {  // the block's other 64 columns are another warp's
+        float amax = block_max(sum, odd);
+        sh.amax[tile_par][warp - 4][lane] = amax;
+        __syncwarp();
+        const int which = j * 4 + quarter;
+        if (lane == 0) bar_arrive(bar_max(which));
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_max(which), tile_par)))) break;
+        amax = fmaxf(amax, sh.amax[tile_par][(warp - 4) ^ 4][lane]);
+        const float inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock,
+                                       row < p.m && inside && !(part & 1));
+        const Wide inv2 = both(inv);
+#pragma unroll
+        for (int q = 0; q < kCols / 2; ++q) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(sum[q]) : "l"(inv2));
+      }
+      if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
       __syncwarp();
       if (lane == 0) bar_arrive(bar_used((it - 1) & 1u));  // (with the last chunk's scales the bias is read too)
     }
@@ -477,26 +494,26 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 constexpr int kFewThreads = 256;  // warp 0 loads, warp 1 issues MMAs, warps 4..7 are the epilogue
 constexpr int kRedPitch = kScaleBlock + 4;
 
-template <int kCols> constexpr int kFewStages = kCols <= 64 ? 4 : 5;
-template <int kCols> constexpr int kFewStageBytes = kOperandBytes + kCols * kScaleBlock;
-template <int kCols> constexpr int kFewSmem = 1024 + kFewStages<kCols> * kFewStageBytes<kCols>;
+template <int kN> constexpr int kFewStages = kN <= 64 ? 4 : 5;
+template <int kN> constexpr int kFewStageBytes = kOperandBytes + kN * kScaleBlock;
+template <int kN> constexpr int kFewSmem = 1024 + kFewStages<kN> * kFewStageBytes<kN>;
 static_assert(kFewSmem<16> - 1024 >= 16 * kRedPitch * 4 && kFewSmem<128> - 1024 >= 128 * kRedPitch * 4, "the sums fit the stages");
 
-template <int kType, int kCols>
-__global__ void __launch_bounds__(kFewThreads, kCols <= 64 ? 2 : 1)
+template <int kType, int kN>
+__global__ void __launch_bounds__(kFewThreads, kN <= 64 ? 2 : 1)
 matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
                   const __grid_constant__ CUtensorMap map_b, int parts) {
   extern __shared__ unsigned char smem_raw[];
-  constexpr int kS = kFewStages<kCols>;
-  constexpr int kTmem = 2 * kCols < 32 ? 32 : 2 * kCols;
+  constexpr int kS = kFewStages<kN>;
+  constexpr int kTmem = 2 * kN < 32 ? 32 : 2 * kN;
   __shared__ __align__(8) Wide s_bar[2 * kS + 4];  // full, empty, accumulator full[2] and read out[2]
-  __shared__ __align__(16) float s_scale[4][2][kCols];
+  __shared__ __align__(16) float s_scale[4][2][kN];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int part = static_cast<int>(blockIdx.x) % parts, n0 = static_cast<int>(blockIdx.x) / parts * kScaleBlock;
-  const int m0 = static_cast<int>(blockIdx.y) * kCols;
+  const int m0 = static_cast<int>(blockIdx.y) * kN;
   const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * part / parts);
   const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (part + 1) / parts);
   unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -537,30 +554,30 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     return false;
   };
 
-  float* s_sum = reinterpret_cast<float*>(smem);  // [kCols][kRedPitch], once the stages are done with
+  float* s_sum = reinterpret_cast<float*>(smem);  // [kN][kRedPitch], once the stages are done with
   if (warp == 0) {
     if (lane == 0) {
       for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
         const int s = it % kS;
         if (!wait_ok(bar_empty(s), ((it / kS) & 1u) ^ 1u)) break;
-        bar_expect(bar_full(s), kFewStageBytes<kCols>);
+        bar_expect(bar_full(s), kFewStageBytes<kN>);
         if (p.starve) continue;
-        load_one(sbase + s * kFewStageBytes<kCols>, &map_b, kb * kScaleBlock, n0, bar_full(s));
-        load_one(sbase + s * kFewStageBytes<kCols> + kOperandBytes, &map_a, kb * kScaleBlock, m0, bar_full(s));
+        load_one(sbase + s * kFewStageBytes<kN>, &map_b, kb * kScaleBlock, n0, bar_full(s));
+        load_one(sbase + s * kFewStageBytes<kN> + kOperandBytes, &map_a, kb * kScaleBlock, m0, bar_full(s));
       }
     }
     __syncwarp();
   } else if (warp == 1) {
     if (lane == 0) {
-      constexpr uint32_t idesc = instr_desc(kScaleBlock, kCols);
+      constexpr uint32_t idesc = instr_desc(kScaleBlock, kN);
       for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
         const int s = it % kS, acc = it & 1;
         if (!wait_ok(bar_read(acc), ((it >> 1) & 1u) ^ 1u) || !wait_ok(bar_full(s), (it / kS) & 1u)) break;
         fence_after();
-        const uint64_t dw = operand_desc(sbase + s * kFewStageBytes<kCols>);
-        const uint64_t dx = operand_desc(sbase + s * kFewStageBytes<kCols> + kOperandBytes);
+        const uint64_t dw = operand_desc(sbase + s * kFewStageBytes<kN>);
+        const uint64_t dx = operand_desc(sbase + s * kFewStageBytes<kN> + kOperandBytes);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma<0>(tmem + acc * kCols, dw + 2u * k, dx + 2u * k, idesc, k > 0);
+        for (int k = 0; k < 4; ++k) mma<0>(tmem + acc * kN, dw + 2u * k, dx + 2u * k, idesc, k > 0);
         commit_one(bar_empty(s));
         commit_one(bar_acc(acc));
       }
@@ -569,10 +586,10 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   } else if (warp >= 4) {
     const int w = warp - 4;
     const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(w * 32) << 16);
-    constexpr int kLoad = kCols < 32 ? kCols : 32, kEach = (kCols + 31) / 32;
-    Wide sum[kCols / 2];
+    constexpr int kLoad = kN < 32 ? kN : 32, kEach = (kN + 31) / 32;
+    Wide sum[kN / 2];
 #pragma unroll
-    for (int q = 0; q < kCols / 2; ++q) sum[q] = 0;
+    for (int q = 0; q < kN / 2; ++q) sum[q] = 0;
     float sa[kEach];
     const int64_t sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
     auto fetch = [&](int kb) {
@@ -580,7 +597,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const int m = m0 + lane + 32 * e;
-        sa[e] = m < p.m && lane + 32 * e < kCols ? scale_value(p.a_scale, static_cast<int64_t>(m) * p.kblocks + kb, p.scale_type) * sb : 0.0f;
+        sa[e] = m < p.m && lane + 32 * e < kN ? scale_value(p.a_scale, static_cast<int64_t>(m) * p.kblocks + kb, p.scale_type) * sb : 0.0f;
       }
     };
     if (kb0 < kb1) fetch(kb0);
@@ -588,25 +605,25 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
       const int acc = it & 1;
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
-        if (lane + 32 * e < kCols) s_scale[w][acc][lane + 32 * e] = sa[e];
+        if (lane + 32 * e < kN) s_scale[w][acc][lane + 32 * e] = sa[e];
       __syncwarp();
       if (kb + 1 < kb1) fetch(kb + 1);
       if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it >> 1) & 1u))) break;
       fence_after();
       const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_scale[w][acc]);
 #pragma unroll
-      for (int c = 0; c < kCols; c += kLoad) {
+      for (int c = 0; c < kN; c += kLoad) {
         uint32_t r[32];
-        if (kCols < 32) {
+        if (kN < 32) {
           asm volatile(
               "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
                 "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-              : "r"(tmem_mine + acc * kCols));
+              : "r"(tmem_mine + acc * kN));
 #pragma unroll
           for (int q = 16; q < 32; ++q) r[q] = 0;
         } else {
-          tmem_ld32(tmem_mine + acc * kCols + c, r);
+          tmem_ld32(tmem_mine + acc * kN + c, r);
         }
         tmem_wait(r);
 #pragma unroll
@@ -624,7 +641,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
     if (!*v_fail) {
 #pragma unroll
-      for (int q = 0; q < kCols / 2; ++q) {
+      for (int q = 0; q < kN / 2; ++q) {
         s_sum[(2 * q) * kRedPitch + w * 32 + lane] = low(sum[q]);
         s_sum[(2 * q + 1) * kRedPitch + w * 32 + lane] = high(sum[q]);
       }
@@ -635,7 +652,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   __syncthreads();
   if (parts > 1) cluster_sync();
   // rows of the result, dealt among the cluster's warps; a warp adds the parts of 128 columns, a lane four neighbours
-  const int rows = p.m - m0 < kCols ? p.m - m0 : kCols;
+  const int rows = p.m - m0 < kN ? p.m - m0 : kN;
   const int n = n0 + 4 * lane;
   if (!*v_fail)
     for (int r = part * (kFewThreads / 32) + warp; r < rows; r += parts * (kFewThreads / 32)) {
@@ -718,23 +735,23 @@ cudaError_t launch_pair(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t s
   return cudaGetLastError();
 }
 
-template <int kType, int kCols>
+template <int kType, int kN>
 cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
   CUtensorMap ma, mb;
-  cudaError_t e = make_map(&ma, q.a, q.m, q.k, q.lda, kCols);
+  cudaError_t e = make_map(&ma, q.a, q.m, q.k, q.lda, kN);
   if (e == cudaSuccess) e = make_map(&mb, q.b, q.n, q.k, q.ldb, kScaleBlock);
-  const void* kernel = reinterpret_cast<const void*>(&matmul_few_kernel<kType, kCols>);
-  if (e == cudaSuccess) e = ensure_dynamic_smem(kernel, kFewSmem<kCols>);
+  const void* kernel = reinterpret_cast<const void*>(&matmul_few_kernel<kType, kN>);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(kernel, kFewSmem<kN>);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = scale_blocks(q.n), rows = (q.m + kCols - 1) / kCols;
+  const int64_t tiles = scale_blocks(q.n), rows = (q.m + kN - 1) / kN;
   if (tiles * 8 > INT32_MAX || rows > 65535) return cudaErrorInvalidConfiguration;
   // parts of K, so that the machine's CTAs have work each
   int parts = 1;
-  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * (kCols <= 64 ? 2 : 1)) parts *= 2;
+  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * (kN <= 64 ? 2 : 1)) parts *= 2;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows));
   cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = kFewSmem<kCols>;
+  cfg.dynamicSmemBytes = kFewSmem<kN>;
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -742,7 +759,7 @@ cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t st
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_few_kernel<kType, kCols>, p, ma, mb, parts);
+  return cudaLaunchKernelEx(&cfg, matmul_few_kernel<kType, kN>, p, ma, mb, parts);
 }
 
 template <int kType>
