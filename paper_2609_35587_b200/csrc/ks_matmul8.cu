@@ -169,40 +169,41 @@ __device__ __forceinline__ Tile tile_at(int64_t t, int tiles_m, int tiles_n) {
 }
 
 // Bias and ReLU on a thread's 64 neighbouring elements of a row.
-__device__ __forceinline__ void finish_block(const MatmulArgs& p, Wide (&sum)[kCols / 2], const float* bias) {
+__device__ __forceinline__ void finish_block(const MatmulArgs& p, float (&sum)[kCols], const float* bias) {
   if (p.bias) {
-    const ulonglong2* b = reinterpret_cast<const ulonglong2*>(bias);
+    const float4* b = reinterpret_cast<const float4*>(bias);
 #pragma unroll
     for (int q = 0; q < kCols / 4; ++q) {
-      const ulonglong2 x = b[q];
-      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q]) : "l"(x.x));
-      asm("add.rn.f32x2 %0, %0, %1;" : "+l"(sum[2 * q + 1]) : "l"(x.y));
+      const float4 x = b[q];
+      sum[4 * q] += x.x;
+      sum[4 * q + 1] += x.y;
+      sum[4 * q + 2] += x.z;
+      sum[4 * q + 3] += x.w;
     }
   }
   if (p.relu) {
 #pragma unroll
-    for (int q = 0; q < kCols / 2; ++q)  // (of what is not a number 0)
-      sum[q] = (static_cast<Wide>(__float_as_uint(fmaxf(high(sum[q]), 0.0f))) << 32) | __float_as_uint(fmaxf(low(sum[q]), 0.0f));
+    for (int q = 0; q < kCols; ++q) sum[q] = fmaxf(sum[q], 0.0f);  // (of what is not a number 0)
   }
 }
 
 // Largest magnitude of them; `odd`: some may be infinite (those do not count).
-__device__ __forceinline__ float block_max(const Wide (&sum)[kCols / 2], bool& odd) {
+__device__ __forceinline__ float block_max(const float (&sum)[kCols], bool& odd) {
   float amax = 0.0f;
 #pragma unroll
-  for (int q = 0; q < kCols / 2; ++q) amax = fmaxf(amax, fmaxf(fabsf(low(sum[q])), fabsf(high(sum[q]))));
+  for (int q = 0; q < kCols; ++q) amax = fmaxf(amax, fabsf(sum[q]));
   odd = amax == __int_as_float(0x7F800000);
   if (odd) {
     amax = 0.0f;
 #pragma unroll
-    for (int q = 0; q < kCols / 2; ++q) amax = fmaxf(amax, fmaxf(finite_abs(low(sum[q])), finite_abs(high(sum[q]))));
+    for (int q = 0; q < kCols; ++q) amax = fmaxf(amax, finite_abs(sum[q]));
   }
   return amax;
 }
 
 // Writes them, rounded to the result's type (e4m3: already scaled).
 template <int kType>
-__device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, const Wide (&sum)[kCols / 2], bool odd, float* s_store) {
+__device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, const float (&sum)[kCols], bool odd, float* s_store) {
   const int lane = threadIdx.x & 31;
   constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
   if (p.wide_rows && n0 + kCols <= p.n) {
@@ -212,14 +213,9 @@ __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0
       uint32_t w[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int c = (g * 8 + i) * kPer;
-        if (kType == KS_E4M3) {
-          const Wide x = sum[c / 2], y = sum[c / 2 + 1 < kCols / 2 ? c / 2 + 1 : 0];
-          w[i] = odd ? e4m3_quad(low(x), high(x), low(y), high(y)) : e4m3_pair_finite(low(x), high(x)) | (e4m3_pair_finite(low(y), high(y)) << 16);
-        } else {
-          const float v[2] = {c & 1 ? high(sum[c / 2]) : low(sum[c / 2]), high(sum[c / 2])};
-          w[i] = pack<kType>(v);
-        }
+        const float* v = sum + (g * 8 + i) * kPer;
+        if (kType == KS_E4M3 && !odd) w[i] = e4m3_pair_finite(v[0], v[1]) | (e4m3_pair_finite(v[2], v[3]) << 16);
+        else w[i] = pack<kType>(v);
       }
       if (row < p.m)
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 32 * g), "r"(w[0]), "r"(w[1]),
@@ -234,10 +230,7 @@ __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0
     if (n0 + c0 >= p.n) break;
     __syncwarp();
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      s_store[lane * kStorePitch + 2 * q] = low(sum[c0 / 2 + q]);
-      s_store[lane * kStorePitch + 2 * q + 1] = high(sum[c0 / 2 + q]);
-    }
+    for (int q = 0; q < 8; ++q) s_store[lane * kStorePitch + q] = sum[c0 + q];
     __syncwarp();
     const int n = n0 + c0 + lane % 8, row0 = row - lane;
     if (n < p.n)
@@ -421,32 +414,30 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
       const Tile at = tile_at(t, tiles_m, tiles_n);
       const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + part * kCols;
       const bool inside = n0 < p.n;  // (of the warp's columns any)
-      Wide sum[kCols / 2];
+      float sum[kCols];
 #pragma unroll
-      for (int q = 0; q < kCols / 2; ++q) sum[q] = 0;
+      for (int q = 0; q < kCols; ++q) sum[q] = 0.0f;
       for (int c = 0; c < chunks && ok; ++c, ++it) {
         const uint32_t buf = it & 1u;
         if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_scale(buf), (it >> 1) & 1u)))) break;
         const int n_kb = p.kblocks - c * kChunk < kChunk ? p.kblocks - c * kChunk : kChunk;
         for (int k = 0; k < n_kb; ++k, ++used) {
           const uint32_t acc = used & 1u;
-          const Wide s = both(sh.a_scale[buf][k][trow] * sh.b_scale[buf][j][k]);
+          const float s = sh.a_scale[buf][k][trow] * sh.b_scale[buf][j][k];
           if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (used >> 1) & 1u)))) break;
           fence_after();
           uint32_t r[32];
           if (inside) {
-            tmem_ld32(tmem_mine + acc * kTile, r);
-            tmem_wait(r);
+            tmem_read32(tmem_mine + acc * kTile, r);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) add_scaled(sum[q], r[2 * q], r[2 * q + 1], s);
-            tmem_ld32(tmem_mine + acc * kTile + 32, r);
-            tmem_wait(r);
+            for (int q = 0; q < 32; ++q) sum[q] = fmaf(__uint_as_float(r[q]), s, sum[q]);
+            tmem_read32(tmem_mine + acc * kTile + 32, r);
           }
           fence_before();
           if (lane == 0) bar_arrive_tmem(read0 + 8u * acc);
           if (inside) {
 #pragma unroll
-            for (int q = 0; q < 16; ++q) add_scaled(sum[16 + q], r[2 * q], r[2 * q + 1], s);
+            for (int q = 0; q < 32; ++q) sum[32 + q] = fmaf(__uint_as_float(r[q]), s, sum[32 + q]);
           }
         }
         if (ok && c + 1 < chunks) {
@@ -467,9 +458,8 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
         amax = fmaxf(amax, sh.amax[tile_par][(warp - 4) ^ 4][lane]);
         const float inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock,
                                        row < p.m && inside && !(part & 1));
-        const Wide inv2 = both(inv);
 #pragma unroll
-        for (int q = 0; q < kCols / 2; ++q) asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(sum[q]) : "l"(inv2));
+        for (int q = 0; q < kCols; ++q) sum[q] *= inv;
       }
       if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
       __syncwarp();
