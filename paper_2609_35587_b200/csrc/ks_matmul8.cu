@@ -246,7 +246,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   extern __shared__ unsigned char smem_raw[];
   // full[kStages] (the leader's are used), empty[kStages], accumulator full[2] and read out[2] (the leader's), scales full[2]
   // and used[2], halves of a block's maxima [8]
-  __shared__ __align__(8) Wide s_bar[2 * kStages + 16];
+  __shared__ __align__(16) Wide s_bar[2 * kStages + 16];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
@@ -406,9 +406,14 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     // warp w owns lanes 32 (w % 4) .. and 64 of a tile's columns, half of block j
     const int quarter = warp & 3, part = (warp - 4) >> 2, j = part >> 1;
     const int trow = quarter * 32 + lane;
-    const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
-    const uint32_t read0 = to_cluster(bar_read(0), 0);
-    uint32_t used = 0, it = 0, tile_par = 0;
+    // the accumulator that comes next: its columns and barriers, of which those of the other differ in one bit
+    uint32_t acc_col = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
+    uint32_t acc_bar = bar_acc(0), read_bar = to_cluster(bar_read(0), 0), acc_parity = 0;
+    const uint32_t first = lane == 0;
+    auto warp_wait = [&](uint32_t bar, uint32_t parity) {
+      return bar_try_warp(bar, parity) || __all_sync(0xFFFFFFFFu, wait_ok(bar, parity));
+    };
+    uint32_t it = 0, tile_par = 0;
     bool ok = true;
     for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
       const Tile at = tile_at(t, tiles_m, tiles_n);
@@ -419,26 +424,28 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
       for (int q = 0; q < kCols; ++q) sum[q] = 0.0f;
       for (int c = 0; c < chunks && ok; ++c, ++it) {
         const uint32_t buf = it & 1u;
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_scale(buf), (it >> 1) & 1u)))) break;
-        const int n_kb = p.kblocks - c * kChunk < kChunk ? p.kblocks - c * kChunk : kChunk;
-        for (int k = 0; k < n_kb; ++k, ++used) {
-          const uint32_t acc = used & 1u;
-          const float s = sh.a_scale[buf][k][trow] * sh.b_scale[buf][j][k];
-          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (used >> 1) & 1u)))) break;
+        if (!(ok = warp_wait(bar_scale(buf), (it >> 1) & 1u))) break;
+        const int n_kb = p.kblocks - c * kChunk;
+        const float *sa = &sh.a_scale[buf][0][trow], *sb = &sh.b_scale[buf][j][0];
+#pragma unroll
+        for (int k = 0; k < kChunk; ++k) {
+          if (k >= n_kb) break;
+          const float s = sa[k * kHalf] * sb[k];
+          if (!(ok = warp_wait(acc_bar, acc_parity))) break;
           fence_after();
           uint32_t r[32];
-          if (inside) {
-            tmem_read32(tmem_mine + acc * kTile, r);
+          tmem_read32(acc_col, r);
 #pragma unroll
-            for (int q = 0; q < 32; ++q) sum[q] = fmaf(__uint_as_float(r[q]), s, sum[q]);
-            tmem_read32(tmem_mine + acc * kTile + 32, r);
-          }
+          for (int q = 0; q < 32; ++q) sum[q] = fmaf(__uint_as_float(r[q]), s, sum[q]);
+          tmem_read32(acc_col + 32, r);
           fence_before();
-          if (lane == 0) bar_arrive_tmem(read0 + 8u * acc);
-          if (inside) {
+          bar_arrive_tmem_if(read_bar, first);
 #pragma unroll
-            for (int q = 0; q < 32; ++q) sum[32 + q] = fmaf(__uint_as_float(r[q]), s, sum[32 + q]);
-          }
+          for (int q = 0; q < 32; ++q) sum[32 + q] = fmaf(__uint_as_float(r[q]), s, sum[32 + q]);
+          acc_parity ^= (acc_bar >> 3) & 1u;  // (after the second of the two)
+          acc_bar ^= 8u;
+          read_bar ^= 8u;
+          acc_col ^= kTile;
         }
         if (ok && c + 1 < chunks) {
           __syncwarp();

@@ -39,16 +39,31 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 __device__ __forceinline__ void bar_arrive_tmem(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-constexpr int kTryNs = 2000;  // how long a try may sleep (without it one lasts some 60 clocks, and the tries take the issue slots of others)
 __device__ __forceinline__ bool bar_try_tmem(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2, %3;\n"
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
       " selp.u32 %0, 1, 0, p;\n}\n"
       : "=r"(ok)
-      : "r"(bar), "r"(parity), "n"(kTryNs)
+      : "r"(bar), "r"(parity)
       : "memory");
   return ok != 0;
+}
+// the same by a whole warp: true in all its lanes or in none
+__device__ __forceinline__ bool bar_try_warp(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p, q;\n mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
+      " vote.sync.all.pred q, p, 0xFFFFFFFF;\n selp.u32 %0, 1, 0, q;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ void bar_arrive_tmem_if(uint32_t cluster_bar, uint32_t mine) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %1, 0;\n @p mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];\n}\n" ::"r"(cluster_bar),
+               "r"(mine)
+               : "memory");
 }
 __device__ __forceinline__ uint32_t to_cluster(uint32_t addr, uint32_t rank) {
   uint32_t r;
