@@ -397,8 +397,8 @@ ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const voi
  * the first candidate in the order of the indices up to which the weights that stay sum to more than u s.
  * Temperature 0: the best candidate (the first of those that share the score), whatever u.
  *   d_scores       device, score_type KS_F32, KS_BF16 or KS_F16. Without d_seg_offsets row i is [i * ld, i * ld + c), ld >= c; with it
- *                  (P + 1 non-decreasing entries) row i is [d_seg_offsets[i], d_seg_offsets[i + 1]), at most 2^31 - 1 long, and
- *                  c and ld are not used
+ *                  (P + 1 non-decreasing entries) row i is [d_seg_offsets[i], d_seg_offsets[i + 1]), c their total length (it
+ *                  decides how the work is shared out, not what is drawn), and ld is not used. A row has at most 2^31 - 1 scores
  *   d_params       device, [P], settings of each row, or NULL: *h_params for all rows. Of d_params a temperature that is not
  *                  above 0 counts as 0, top_k < 1 as 0, top_p not below 1 as 1, min_p not above 0 as 0
  *   d_u            device, [P][draws] fp32; below 0 counts as 0, from 1 on as the largest below 1. 1 <= draws <= KS_MAX_K
@@ -408,7 +408,7 @@ ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const voi
  * number); what lies below half of that is never drawn. Draws do not depend on how the work is shared out: the same call gives the same bits. Asynchronous on
  * `stream`; no workspace. KS_ERR_INVALID_ARG for draws out of range, a negative size, or *h_params with a setting that is no number,
  * negative, or top_p outside (0, 1], min_p above 1. */
-ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int c, int64_t ld, const int64_t* d_seg_offsets,
+ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int64_t c, int64_t ld, const int64_t* d_seg_offsets,
                     const ks_sampling* h_params, const ks_sampling* d_params, const float* d_u, int draws, int32_t* d_idx,
                     float* d_logp, void* stream);
 

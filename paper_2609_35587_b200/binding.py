@@ -104,7 +104,7 @@ def _load() -> ctypes.CDLL:
     lib.ks_debug_split_walks.restype = i64
     lib.ks_quantize_e4m3.argtypes = [vp, vp, i32, i64, i64, i64, i32, i32, vp, i64, vp, vp]
     lib.ks_matmul_e4m3.argtypes = [vp, vp, i64, vp, vp, i64, vp, i32, i64, i64, i64, vp, i32, vp, i64, i32, vp, vp]
-    lib.ks_sample.argtypes = [vp, vp, i32, i32, i32, i64, vp, ctypes.POINTER(_Sampling), vp, vp, i32, vp, vp, vp]
+    lib.ks_sample.argtypes = [vp, vp, i32, i32, i64, i64, vp, ctypes.POINTER(_Sampling), vp, vp, i32, vp, vp, vp]
     lib.ks_debug_bounds_line.restype = i32
     lib.ks_debug_bounds_clear.restype = None
     for name in EXPORTS:
@@ -541,7 +541,7 @@ class Context:
         else:
             if d_seg_off.dtype != torch.int64 or d_seg_off.shape != (P + 1,):
                 raise ValueError("sample: d_seg_off")
-            sp, ld, c = _dptr(scores), 0, 0
+            sp, ld, c = _dptr(scores), 0, scores.numel()
         if params is not None and params.numel() * params.element_size() != 16 * P:
             raise ValueError("sample: params")
         if out_idx is None:

@@ -875,11 +875,11 @@ ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const voi
   return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_matmul_e4m3");
 }
 
-ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int c, int64_t ld, const int64_t* d_seg_offsets,
+ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int64_t c, int64_t ld, const int64_t* d_seg_offsets,
                     const ks_sampling* h_params, const ks_sampling* d_params, const float* d_u, int draws, int32_t* d_idx,
                     float* d_logp, void* stream) {
   if (!ctx || P < 0 || draws < 1 || draws > KS_MAX_K || score_type < KS_F32 || score_type > KS_F16) return KS_ERR_INVALID_ARG;
-  if (!d_seg_offsets && (c < 0 || ld < c)) return KS_ERR_INVALID_ARG;
+  if (c < 0 || (!d_seg_offsets && (ld < c || c > kMaxExtent))) return KS_ERR_INVALID_ARG;
   if (!d_params) {  // (comparisons that a value that is no number does not pass)
     if (!h_params || !(h_params->temperature >= 0.0f) || !std::isfinite(h_params->temperature) || h_params->top_k < 0 ||
         !(h_params->top_p > 0.0f && h_params->top_p <= 1.0f) || !(h_params->min_p >= 0.0f && h_params->min_p <= 1.0f))
@@ -891,6 +891,7 @@ ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, in
   DeviceGuard g(ctx->device);
   const ks::SampleArgs a{d_scores, ld, d_seg_offsets, P, c, d_params ? ks_sampling{} : *h_params, d_params, d_u, draws, d_idx, d_logp};
   cudaError_t e = ks::launch_sample(a, score_type, static_cast<cudaStream_t>(stream), &ctx->launches);
+  if (e == cudaErrorInvalidConfiguration) return KS_ERR_UNSUPPORTED;
   return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_sample");
 }
 

@@ -372,8 +372,7 @@ struct SampleArgs {
   const void* scores;
   int64_t ld;
   const int64_t* seg_off;
-  int64_t p;
-  int c;
+  int64_t p, c;
   ks_sampling all;
   const ks_sampling* params;
   const float* u;

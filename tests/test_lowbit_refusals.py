@@ -71,7 +71,7 @@ def sample(**kw):
 
 
 @pytest.mark.parametrize("bad", [
-    dict(scores=None), dict(u=None), dict(idx=None), dict(P=-1), dict(c=-1), dict(ld=9), dict(draws=0), dict(draws=33), dict(score_type=3),
+    dict(scores=None), dict(u=None), dict(idx=None), dict(P=-1), dict(c=-1), dict(ld=9), dict(c=1 << 31, ld=1 << 31), dict(seg=P, c=-1), dict(draws=0), dict(draws=33), dict(score_type=3),
     dict(score_type=-1), dict(scores=P + 2), dict(params=P + 2), dict(seg=P + 4), dict(none=True), dict(t=-1.0), dict(t=float("nan")),
     dict(t=float("inf")), dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1),
     dict(min_p=float("nan"))])
