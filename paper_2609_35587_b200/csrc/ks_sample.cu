@@ -29,22 +29,41 @@ constexpr int kBins = 2048;
 constexpr int kList = 1024;        // candidates of a bin that are sorted
 constexpr int kMaxCtas = 16;       // of a cluster
 constexpr int kLoads = 8;          // 16-byte loads that a thread keeps: two CTAs an SM
-constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (52 bits)
+constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (51 bits)
 constexpr int kDigit = 11;         // bits of (score, index) that a bin is narrowed down by
 
 struct Row {
-  float best, bins;   // bins a unit of score
-  float t;
-  double inv_t;
+  float best;
+  float reach;        // scores further below the best one have no weight
+  float bins;         // bins a unit of score
+  double best_wide;
+  double steps;       // 64ths of a power of two a unit of score
   double one;         // weight of the best score, 2^s
   double least;       // weights below do not stay (min-p)
 };
 
-// Weight in units of 2^-s before it is rounded; the best score's is exact, also where it is infinite.
-__device__ __forceinline__ double scaled_weight(const Row& r, float x) {
-  return x == r.best ? r.one : exp((static_cast<double>(x) - static_cast<double>(r.best)) * r.inv_t) * r.one;
+// Weight of a score within reach in units of 2^-s, before it is rounded: 2^(n / 64) from a table of 64 (times 2^s) and the
+// exponent, times the exponential of what is left, at most ln 2 / 128, by its series (P. T. P. Tang's table-driven method, ACM
+// TOMS 15, 1989). The first term that is left out is below 2^-54. The best score's weight is exact, also where it is infinite.
+__device__ __forceinline__ double scaled_weight(const Row& r, const double* table, float x) {
+  constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to a whole number in the low word
+  constexpr double kL = 0.69314718055994530942 / 64.0;
+  const double z = (static_cast<double>(x) - r.best_wide) * r.steps, m = z + kRound;
+  const int n = __double2loint(m);
+  const double f = z - (m - kRound);
+  double e = fma(f, kL * kL * kL * kL * kL / 120.0, kL * kL * kL * kL / 24.0);
+  e = fma(f, e, kL * kL * kL / 6.0);
+  e = fma(f, e, kL * kL / 2.0);
+  e = fma(f, e, kL);
+  e = fma(f, e, 1.0);
+  const double w = table[n & 63] * e;
+  const double v = __hiloint2double(__double2hiint(w) + ((n >> 6) << 20), __double2loint(w));
+  return x == r.best ? r.one : v;
 }
-__device__ __forceinline__ Wide whole(double w) { return static_cast<Wide>(__double2ll_rn(w)); }
+// rounded; w <= 2^51, so that the sum's low bits are the whole number
+__device__ __forceinline__ Wide whole(double w) {
+  return static_cast<Wide>(__double_as_longlong(w + 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
+}
 
 __device__ __forceinline__ int bin_of(const Row& r, float x) {
   return static_cast<int>(fminf((r.best - x) * r.bins, static_cast<float>(kBins - 1)));
@@ -77,13 +96,33 @@ __device__ __forceinline__ Wide block_scan(Wide v, Wide* s_warp, Wide& total) {
   return (warp > 0 ? before : 0) + in - v;
 }
 
+// The same of two numbers at once.
+__device__ __forceinline__ void block_scan2(Wide& v, Wide& w, Wide (*s_warp)[kWarps], Wide& total_v, Wide& total_w) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const Wide in_v = warp_scan(v, lane), in_w = warp_scan(w, lane);
+  __syncthreads();
+  if (lane == 31) {
+    s_warp[0][warp] = in_v;
+    s_warp[1][warp] = in_w;
+  }
+  __syncthreads();
+  const Wide all_v = warp_scan(lane < kWarps ? s_warp[0][lane] : 0, lane), all_w = warp_scan(lane < kWarps ? s_warp[1][lane] : 0, lane);
+  total_v = __shfl_sync(0xFFFFFFFFu, all_v, kWarps - 1);
+  total_w = __shfl_sync(0xFFFFFFFFu, all_w, kWarps - 1);
+  const Wide before_v = __shfl_sync(0xFFFFFFFFu, all_v, warp > 0 ? warp - 1 : 0);
+  const Wide before_w = __shfl_sync(0xFFFFFFFFu, all_w, warp > 0 ? warp - 1 : 0);
+  v = (warp > 0 ? before_v : 0) + in_v - v;
+  w = (warp > 0 ? before_w : 0) + in_w - w;
+}
+
 struct Shared {
+  double table[64];
   unsigned count[kBins];
-  Wide sum[kBins];
+  unsigned low[kBins], high[kBins];  // of a bin's sum
   unsigned m_count[kBins / 2];  // this CTA's share of the bins, over the cluster
   Wide m_sum[kBins / 2];
   Wide list[kList];
-  Wide warp[kWarps];
+  Wide warp[kWarps], warp2[2][kWarps];
   // what the cluster's other CTAs read
   Wide best;
   float least[kWarps], min;
@@ -149,24 +188,30 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const int held = kThreads * V * loads;
   const int tiles = first < last ? static_cast<int>((last - first + held - 1) / held) : 0;
 
-  // The V scores from a place of this CTA's on; what lies outside its stretch as -inf.
+  // The V scores from a place of this CTA's on; what lies outside its stretch, and what is no number, as -inf, and of the two
+  // zeros one.
   auto fetch = [&](int64_t at) {
     uint4 w;
+    T t[V];
     if (at >= shift && at + V <= last) {
       w = __ldg(reinterpret_cast<const uint4*>(base + at));
+      memcpy(t, &w, 16);
     } else {
-      T t[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) t[v] = at + v >= shift && at + v < last ? base[at + v] : from_float<T>(none);
-      memcpy(&w, t, 16);
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float y = to_float(t[v]) + 0.0f;
+      t[v] = from_float<T>(y == y ? y : none);
+    }
+    memcpy(&w, t, 16);
     return w;
   };
   auto score = [&](const uint4& w, int v) {
     T t[V];
     memcpy(t, &w, 16);
-    const float y = to_float(t[v]) + 0.0f;  // (of the two zeros one)
-    return y == y ? y : none;
+    return to_float(t[v]);
   };
   // Place of a thread's load in a tile: the loads of a warp are neighbours, and warps follow one another.
   auto place = [&](int tile, int q) { return first + static_cast<int64_t>(tile) * held + (static_cast<int64_t>(warp) * loads + q) * (32 * V) + lane * V; };
@@ -207,20 +252,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       }
     }
   }
-  Wide best = 0;
-  // (the first of several that share the score)
-  if (__any_sync(0xFFFFFFFFu, top > none)) {
-    const float warp_top = fmaxf(top, none);
-    float highest = warp_top;
-#pragma unroll
-    for (int d = 16; d > 0; d /= 2) highest = fmaxf(highest, __shfl_xor_sync(0xFFFFFFFFu, highest, d));
-    if (top == highest) {
-      unsigned at = 0xFFFFFFFFu;
-      each([&](int64_t i, float y) {
-        if (y == top) at = min(at, static_cast<unsigned>(i - shift));
-      });
-      best = make_key(top, static_cast<int>(at));
-    }
+  // Temperature 0 is the limit of small ones: the best candidate alone, of several that share its score the first.
+  const bool greedy = !(set.temperature > 0.0f);
+  Wide best = top > none ? make_key(top, 0) : 0;
+  if (greedy && top > none) {
+    unsigned at = 0xFFFFFFFFu;
+    each([&](int64_t i, float y) {
+      if (y == top) at = min(at, static_cast<unsigned>(i - shift));
+    });
+    best = make_key(top, static_cast<int>(at));
   }
 #pragma unroll
   for (int d = 16; d > 0; d /= 2) {
@@ -248,10 +288,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       s.listed = 0;
     }
   }
-  for (int i = threadIdx.x; i < kBins; i += kThreads) {
-    s.count[i] = 0;
-    s.sum[i] = 0;
-  }
+  for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.low[i] = s.high[i] = 0;
   meet(ctas);
   best = 0;
   for (int r = 0; r < ctas; ++r) {
@@ -269,42 +306,44 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     return;
   }
 
-  // Temperature 0 is the limit of small ones: the best candidate alone.
-  const bool greedy = !(set.temperature > 0.0f);
   Row r;
   r.best = key_score(best);
-  r.t = set.temperature;
-  r.inv_t = greedy ? 0.0 : 1.0 / static_cast<double>(set.temperature);
-  r.one = ldexp(1.0, min(52, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
+  r.best_wide = static_cast<double>(r.best);
+  r.steps = greedy ? 0.0 : 64.0 * 1.4426950408889634074 / static_cast<double>(set.temperature);
+  r.one = ldexp(1.0, min(51, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
   r.least = set.min_p > 0.0f ? fmin(static_cast<double>(set.min_p), 1.0) * r.one : 0.0;
+  r.reach = greedy ? 0.0f : (kReach + 1.0f) * set.temperature;
   // bins over what the scores reach, but no further than weights do
-  const float reach = fminf(r.best - low, kReach * set.temperature);
-  r.bins = reach > 0.0f ? static_cast<float>(kBins - 1) / reach : 0.0f;
-  Wide cut = greedy ? best : 0;  // keys from here on stay
+  const float span = fminf(r.best - low, kReach * set.temperature);
+  r.bins = span > 0.0f ? static_cast<float>(kBins - 1) / span : 0.0f;
+  if (threadIdx.x < 64) s.table[threadIdx.x] = exp2(threadIdx.x / 64.0) * r.one;
+  __syncthreads();
+  // what stays: scores above `cut_score`, and those that equal it up to the place `cut_at`
+  Wide cut = greedy ? best : 0;
+  auto weight = [&](float y) { return whole(scaled_weight(r, s.table, y)); };
 
   // ---- cuts ----
   bool counted = false;  // the histogram over all candidates is there, over the cluster
   const int mine = kBins / ctas, per = (mine + kThreads - 1) / kThreads;  // bins of this CTA, and of a thread
   const unsigned* m_count = ctas == 1 ? s.count : s.m_count;
-  const Wide* m_sum = ctas == 1 ? s.sum : s.m_sum;
+  auto m_sum = [&](int i) { return ctas == 1 ? (static_cast<Wide>(s.high[i]) << 32) + s.low[i] : s.m_sum[i]; };
   // histogram of the candidates that `digit` gives a bin (-1: none), and this CTA's share of it over the cluster
   auto histogram = [&](bool clear, auto digit) {
     if (clear) {
-      for (int i = threadIdx.x; i < kBins; i += kThreads) {
-        s.count[i] = 0;
-        s.sum[i] = 0;
-      }
+      for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.low[i] = s.high[i] = 0;
       __syncthreads();
     }
     each([&](int64_t i, float y) {
-      // (what lies behind the reach of weights has none; the rounding of this comparison does not matter there)
-      if ((r.best - y) * static_cast<float>(r.inv_t) > kReach + 1.0f) return;
-      const Wide w = whole(scaled_weight(r, y));
+      if (r.best - y > r.reach) return;
+      const Wide w = weight(y);
       if (w == 0) return;
       const int d = digit(i, y);
       if (d < 0) return;
       atomicAdd(&s.count[d], 1u);
-      atomicAdd(&s.sum[d], w);
+      // 64 bits in two additions of 32: who sees the low one wrap carries
+      const unsigned add = static_cast<unsigned>(w), was = atomicAdd(&s.low[d], add);
+      const unsigned up = static_cast<unsigned>(w >> 32) + (was + add < was ? 1u : 0u);
+      if (up) atomicAdd(&s.high[d], up);
     });
     meet(ctas);
     Wide c = 0, w = 0;
@@ -314,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         Wide bw = 0;
         for (int o = 0; o < ctas; ++o) {
           bc += *of_rank(&s.count[rank * mine + i], o, ctas);
-          bw += *of_rank(&s.sum[rank * mine + i], o, ctas);
+          bw += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
         }
         s.m_count[i] = bc;
         s.m_sum[i] = bw;
@@ -324,11 +363,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     else
       for (int i = threadIdx.x; i < mine; i += kThreads) {
         c += m_count[i];
-        w += m_sum[i];
+        w += m_sum(i);
       }
     Wide total_c, total_w;
-    block_scan(c, s.warp, total_c);
-    block_scan(w, s.warp, total_w);
+    block_scan2(c, w, s.warp2, total_c, total_w);
     if (threadIdx.x == 0) {
       s.share_count = total_c;
       s.share_sum = total_w;
@@ -372,20 +410,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
         }
       }
       if (rank == owner) {
-        Wide tc = 0, tw = 0, total;
+        Wide bc = 0, bw = 0, total_c, total_w;
         for (int q = 0; q < per; ++q) {
           const int i = threadIdx.x * per + q;
           if (i < mine) {
-            tc += m_count[i];
-            tw += m_sum[i];
+            bc += m_count[i];
+            bw += m_sum(i);
           }
         }
-        Wide bc = block_scan(tc, s.warp, total) + own_c, bw = block_scan(tw, s.warp, total) + own_w;
+        block_scan2(bc, bw, s.warp2, total_c, total_w);
+        bc += own_c;
+        bw += own_w;
         for (int q = 0; q < per; ++q) {
           const int i = threadIdx.x * per + q;
           if (i >= mine) break;
           const bool starts = n > 0 ? bc < n : static_cast<double>(bw) < target;
-          const bool ends = n > 0 ? bc + m_count[i] >= n : static_cast<double>(bw + m_sum[i]) >= target;
+          const bool ends = n > 0 ? bc + m_count[i] >= n : static_cast<double>(bw + m_sum(i)) >= target;
           if (m_count[i] > 0 && starts && ends) {
             s.bin = rank * mine + i;
             s.held = m_count[i];
@@ -393,7 +433,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
             s.before_sum = bw;
           }
           bc += m_count[i];
-          bw += m_sum[i];
+          bw += m_sum(i);
         }
       }
       meet(ctas);
@@ -405,14 +445,14 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       if (level == 0) bin0 = bin;
       else prefix |= static_cast<Wide>(kBins - 1 - bin) << (shift_now > 0 ? shift_now : 0);
       auto member = [&](Wide key, float y) {
-        return key >= outer && bin_of(r, y) == bin0 && (level == 0 || (key >> (shift_now > 0 ? shift_now : 0)) == (prefix >> (shift_now > 0 ? shift_now : 0)));
+        return bin_of(r, y) == bin0 && key >= outer && (level == 0 || (key >> (shift_now > 0 ? shift_now : 0)) == (prefix >> (shift_now > 0 ? shift_now : 0)));
       };
       if (held <= kList) {
         unsigned* n_list = of_rank(&s.listed, owner, ctas);
         Wide* list = of_rank(&s.list[0], owner, ctas);
         each([&](int64_t i, float y) {
           const Wide key = key_of(i, y);
-          if (!member(key, y) || whole(scaled_weight(r, y)) == 0) return;
+          if (!member(key, y) || r.best - y > r.reach || weight(y) == 0) return;
           list[atomicAdd(n_list, 1u)] = key;
         });
         meet(ctas);
@@ -424,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
 #pragma unroll
           for (int q = 0; q < kEach; ++q) {
             const int i = threadIdx.x * kEach + q;
-            w2[q] = i < n_held ? whole(scaled_weight(r, key_score(s.list[i]))) : 0;
+            w2[q] = i < n_held ? weight(key_score(s.list[i])) : 0;
             sum2 += w2[q];
           }
           Wide bw = block_scan(sum2, s.warp, total) + base_sum;
@@ -468,11 +508,13 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   }
 
   // ---- the sum of what stays, then the draws, in the order of the indices ----
+  const float cut_score = cut > 0 ? key_score(cut) : none;
+  const unsigned cut_at = cut > 0 ? static_cast<unsigned>(key_index(cut)) : 0xFFFFFFFFu;
   auto stays = [&](int64_t i, float y) -> Wide {
-    if (!(y > none) || (cut > 0 && key_of(i, y) < cut)) return 0;
+    if (!(y > cut_score) && !(y == cut_score && y > none && static_cast<unsigned>(i - shift) <= cut_at)) return 0;
     if (greedy) return 1;
-    if ((r.best - y) * static_cast<float>(r.inv_t) > kReach + 1.0f) return 0;
-    const double w = scaled_weight(r, y);
+    if (r.best - y > r.reach) return 0;
+    const double w = scaled_weight(r, s.table, y);
     return w >= r.least ? whole(w) : 0;
   };
   Wide sum = 0;
@@ -523,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
               const float y = score(raw, v);
               a.idx[p * a.draws + q_draw] = static_cast<int32_t>(i0 + v - shift);
               if (a.logp) {
-                const double d = y == r.best ? 0.0 : (static_cast<double>(y) - static_cast<double>(r.best)) * r.inv_t;
+                const double d = y == r.best ? 0.0 : (static_cast<double>(y) - r.best_wide) / static_cast<double>(set.temperature);
                 a.logp[p * a.draws + q_draw] = static_cast<float>(d - log_all);
               }
             }
