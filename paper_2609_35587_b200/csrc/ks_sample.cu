@@ -9,8 +9,10 @@
 // place in it. A histogram over the distance to the best score narrows it down to one bin, in which some hundred candidates
 // lie; they are sorted. Bins that hold more are narrowed down further by the bits of (score, index).
 //
-// A row belongs to a cluster of 1 to 16 CTAs that keep its scores in shared memory, each thread its own (rows longer than the
-// cluster holds are read again in every phase), so that a row is read from memory once. The CTAs' results meet there too.
+// A row of a call with few rows belongs to a cluster of up to 16 CTAs that keep its scores in shared memory, each thread its
+// own; the CTAs' results meet there too. Where there are rows for the whole machine a CTA takes a row by itself and reads it
+// again in every phase, mostly from L2: four smaller CTAs an SM hide each other's barriers, of which a cluster has more and
+// longer ones (1,024 x 60,000 scores: 947 us by clusters of 4).
 #include <algorithm>
 #include <cmath>
 
@@ -24,13 +26,19 @@ namespace {
 
 using Wide = unsigned long long;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 2048;
+// (what is not inlined passes a load's scores through memory)
+#define KS_INLINE __attribute__((always_inline))
+
+template <typename T> constexpr bool is_bf16 = false;
+template <> constexpr bool is_bf16<__nv_bfloat16> = true;
+
+constexpr int kBins = 1024;
 constexpr int kList = 1024;        // candidates of a bin that are sorted
 constexpr int kMaxCtas = 16;       // of a cluster
-constexpr int kLoads = 8;          // 16-byte loads that a thread keeps: two CTAs an SM
+constexpr int kHeldLoads = 8;      // 16-byte loads that a thread keeps at most
+constexpr int kEntries = 1024;     // sums over stretches of a row that a CTA keeps
 constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (51 bits)
-constexpr int kDigit = 11;         // bits of (score, index) that a bin is narrowed down by
+constexpr int kDigit = 10;         // bits of (score, index) that a bin is narrowed down by
 
 struct Row {
   float best;
@@ -84,7 +92,8 @@ __device__ __forceinline__ Wide warp_sum(Wide v) {
 }
 
 // Exclusive sum over the block's threads; the block's in `total`.
-__device__ __forceinline__ Wide block_scan(Wide v, Wide* s_warp, Wide& total) {
+template <int kWarps>
+__device__ __forceinline__ Wide block_scan(Wide v, Wide (&s_warp)[kWarps], Wide& total) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const Wide in = warp_scan(v, lane);
   __syncthreads();
@@ -97,7 +106,8 @@ __device__ __forceinline__ Wide block_scan(Wide v, Wide* s_warp, Wide& total) {
 }
 
 // The same of two numbers at once.
-__device__ __forceinline__ void block_scan2(Wide& v, Wide& w, Wide (*s_warp)[kWarps], Wide& total_v, Wide& total_w) {
+template <int kWarps>
+__device__ __forceinline__ void block_scan2(Wide& v, Wide& w, Wide (&s_warp)[2][kWarps], Wide& total_v, Wide& total_w) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const Wide in_v = warp_scan(v, lane), in_w = warp_scan(w, lane);
   __syncthreads();
@@ -115,6 +125,7 @@ __device__ __forceinline__ void block_scan2(Wide& v, Wide& w, Wide (*s_warp)[kWa
   w = (warp > 0 ? before_w : 0) + in_w - w;
 }
 
+template <int kWarps>
 struct Shared {
   double table[64];
   unsigned count[kBins];
@@ -145,6 +156,7 @@ __device__ __forceinline__ void meet(int ctas) {
 }
 
 // The block's list of n <= kList keys, descending.
+template <int kThreads>
 __device__ __forceinline__ void sort_list(Wide* list, int n) {
   int size = 64;
   while (size < n) size *= 2;
@@ -160,15 +172,50 @@ __device__ __forceinline__ void sort_list(Wide* list, int n) {
           list[b] = x;
         }
       }
-      if (j > 32 || j == 1) __syncthreads();
+      if (j > 32 || j == 1) __syncthreads();  // (from 32 down a warp's pairs are its own)
       else __syncwarp();
     }
 }
 
+// The scores of one load, with what is no number as -inf and of the two zeros one.
+__device__ __forceinline__ float normal(float y) { return fmaxf(y + 0.0f, __int_as_float(0xFF800000)); }
+__device__ __forceinline__ void unpack(const uint4& w, float (&y)[4], float) {
+  y[0] = normal(__uint_as_float(w.x));
+  y[1] = normal(__uint_as_float(w.y));
+  y[2] = normal(__uint_as_float(w.z));
+  y[3] = normal(__uint_as_float(w.w));
+}
+__device__ __forceinline__ void unpack(const uint4& w, float (&y)[8], __nv_bfloat16) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = normal(__uint_as_float(u[i] << 16));
+    y[2 * i + 1] = normal(__uint_as_float(u[i] & 0xFFFF0000u));
+  }
+}
+__device__ __forceinline__ void unpack(const uint4& w, float (&y)[8], __half) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+    y[2 * i] = normal(f.x);
+    y[2 * i + 1] = normal(f.y);
+  }
+}
+// Four bytes of a load: scores where `live` says so, -inf elsewhere.
+__device__ __forceinline__ uint32_t word_of(const float* base, bool live) { return live ? __float_as_uint(*base) : 0xFF800000u; }
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_constant__ SampleArgs a, int ctas, int loads) {
-  __shared__ Shared s;
-  extern __shared__ uint4 s_held[];  // [loads][threads]
+__device__ __forceinline__ uint32_t word_of(const T* base, bool live0, bool live1, uint32_t none) {
+  const uint32_t lo = live0 ? *reinterpret_cast<const uint16_t*>(base) : none;
+  const uint32_t hi = live1 ? *reinterpret_cast<const uint16_t*>(base + 1) : none;
+  return lo | (hi << 16);
+}
+
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const __grid_constant__ SampleArgs a, int ctas, int held_loads) {
+  constexpr int kWarps = kThreads / 32;
+  __shared__ Shared<kWarps> s;
+  extern __shared__ uint4 s_held[];  // [held_loads][threads]
   constexpr int V = 16 / static_cast<int>(sizeof(T));  // scores a load
   const int rank = ctas == 1 ? 0 : static_cast<int>(blockIdx.x) % ctas;
   const int64_t p = blockIdx.x / ctas;
@@ -179,86 +226,83 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   const ks_sampling set = a.params ? a.params[p] : a.all;
   const float none = __int_as_float(0xFF800000);
 
-  // This CTA's stretch of the row, in places that are counted from the last 16-byte boundary at or before its first score.
+  // This CTA's stretch of the row, in places that are counted from the last 16-byte boundary at or before its first score. It
+  // is kept in shared memory where it fits, one tile, else read again in every phase, in tiles that are few enough for the
+  // sums over their warps' parts to be kept.
   const int shift = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
   const T* base = row - shift;
   const int64_t places = static_cast<int64_t>(len) + shift;
   const int64_t chunk = ((places + ctas - 1) / ctas + 32 * V - 1) / (32 * V) * (32 * V);
   const int64_t first = rank * chunk, last = first + chunk < places ? first + chunk : places;
-  const int held = kThreads * V * loads;
-  const int tiles = first < last ? static_cast<int>((last - first + held - 1) / held) : 0;
+  const int64_t all_loads = first < last ? (last - first + kThreads * V - 1) / (kThreads * V) : 0;
+  const bool held = all_loads <= held_loads;
+  const int64_t least_loads = (all_loads + kEntries / kWarps - 1) / (kEntries / kWarps);
+  const int loads = static_cast<int>(held ? all_loads : least_loads > kHeldLoads ? least_loads : kHeldLoads);
+  const int tiles = loads > 0 ? static_cast<int>((all_loads + loads - 1) / loads) : 0;
 
-  // The V scores from a place of this CTA's on; what lies outside its stretch, and what is no number, as -inf, and of the two
-  // zeros one.
-  auto fetch = [&](int64_t at) {
-    uint4 w;
-    T t[V];
-    if (at >= shift && at + V <= last) {
-      w = __ldg(reinterpret_cast<const uint4*>(base + at));
-      memcpy(t, &w, 16);
-    } else {
+  auto fetch = [&](int64_t at) KS_INLINE {  // the load of V scores at a place; what lies outside the stretch as -inf
+    if (at >= shift && at + V <= last) return __ldg(reinterpret_cast<const uint4*>(base + at));
+    uint32_t u[4];
 #pragma unroll
-      for (int v = 0; v < V; ++v) t[v] = at + v >= shift && at + v < last ? base[at + v] : from_float<T>(none);
+    for (int i = 0; i < 4; ++i) {
+      const int64_t e = at + i * (V / 4);
+      const bool live0 = e >= shift && e < last, live1 = e + 1 >= shift && e + 1 < last;
+      if constexpr (V == 4) u[i] = word_of(reinterpret_cast<const float*>(base + e), live0);
+      else u[i] = word_of(base + e, live0, live1, sizeof(T) == 2 && is_bf16<T> ? 0xFF80u : 0xFC00u);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float y = to_float(t[v]) + 0.0f;
-      t[v] = from_float<T>(y == y ? y : none);
-    }
-    memcpy(&w, t, 16);
-    return w;
+    return make_uint4(u[0], u[1], u[2], u[3]);
   };
-  auto score = [&](const uint4& w, int v) {
-    T t[V];
-    memcpy(t, &w, 16);
-    return to_float(t[v]);
+  // Place of a load: those of a warp are neighbours, and warps follow one another in a tile.
+  auto place = [&](int tile, int w, int q) KS_INLINE {
+    return first + ((static_cast<int64_t>(tile) * kWarps + w) * loads + q) * (32 * V) + lane * V;
   };
-  // Place of a thread's load in a tile: the loads of a warp are neighbours, and warps follow one another.
-  auto place = [&](int tile, int q) { return first + static_cast<int64_t>(tile) * held + (static_cast<int64_t>(warp) * loads + q) * (32 * V) + lane * V; };
-  auto get = [&](int tile, int q) { return tiles == 1 ? s_held[q * kThreads + threadIdx.x] : fetch(place(tile, q)); };
-  auto key_of = [&](int64_t at, float y) { return make_key(y, static_cast<int>(at - shift)); };
-  // f(place, score) for all scores of this thread that are not -inf
-  auto each = [&](auto f) {
-    for (int tile = 0; tile < tiles; ++tile)
+  auto get = [&](int tile, int w, int q) KS_INLINE { return held ? s_held[q * kThreads + w * 32 + lane] : fetch(place(tile, w, q)); };
+  auto key_of = [&](int64_t at, float y) KS_INLINE { return make_key(y, static_cast<int>(at - shift)); };
+  // f(place, scores) for all loads of this thread
+  auto each = [&](auto f) KS_INLINE {
+    for (int tile = 0; tile < tiles; ++tile) {
+      int64_t at = place(tile, warp, 0);
+      uint4 next = get(tile, warp, 0);
 #pragma unroll 1
-      for (int q = 0; q < loads; ++q) {
-        const int64_t at = place(tile, q);
-        if (at - lane * V >= last) break;
-        const uint4 w = get(tile, q);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const float y = score(w, v);
-          if (y > none) f(at + v, y);
-        }
+      for (int q = 0; q < loads && at - lane * V < last; ++q, at += 32 * V) {
+        float y[V];
+        unpack(next, y, T{});
+        if (q + 1 < loads) next = get(tile, warp, q + 1);  // on its way while these are worked on
+        f(at, y);
       }
+    }
   };
 
   // ---- the best candidate, and the least score that is a number ----
   float top = none, low = __int_as_float(0x7F800000);
-  for (int tile = 0; tile < tiles; ++tile) {
-    uint4 w[kLoads];
+  for (int tile = 0; tile < tiles; ++tile)
+    for (int q0 = 0; q0 < loads; q0 += 4) {
+      uint4 w[4];
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q)
-      if (q < loads) w[q] = fetch(place(tile, q));
+      for (int q = 0; q < 4; ++q)
+        if (q0 + q < loads) w[q] = fetch(place(tile, warp, q0 + q));
 #pragma unroll
-    for (int q = 0; q < kLoads; ++q) {
-      if (q >= loads) break;
-      if (tiles == 1) s_held[q * kThreads + threadIdx.x] = w[q];
+      for (int q = 0; q < 4; ++q) {
+        if (q0 + q >= loads) break;
+        if (held) s_held[(q0 + q) * kThreads + threadIdx.x] = w[q];
+        float y[V];
+        unpack(w[q], y, T{});
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const float y = score(w[q], v);
-        top = fmaxf(top, y);
-        if (y > none) low = fminf(low, y);
+        for (int v = 0; v < V; ++v) {
+          top = fmaxf(top, y[v]);
+          low = fminf(low, y[v] > none ? y[v] : low);
+        }
       }
     }
-  }
   // Temperature 0 is the limit of small ones: the best candidate alone, of several that share its score the first.
   const bool greedy = !(set.temperature > 0.0f);
   Wide best = top > none ? make_key(top, 0) : 0;
   if (greedy && top > none) {
     unsigned at = 0xFFFFFFFFu;
-    each([&](int64_t i, float y) {
-      if (y == top) at = min(at, static_cast<unsigned>(i - shift));
+    each([&](int64_t i, const float (&y)[V]) KS_INLINE {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (y[v] == top) at = min(at, static_cast<unsigned>(i + v - shift));
     });
     best = make_key(top, static_cast<int>(at));
   }
@@ -320,30 +364,37 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   __syncthreads();
   // what stays: scores above `cut_score`, and those that equal it up to the place `cut_at`
   Wide cut = greedy ? best : 0;
-  auto weight = [&](float y) { return whole(scaled_weight(r, s.table, y)); };
+  // (without a branch: what lies behind the reach of weights, -inf above all, computes something and gets 0)
+  auto weight = [&](float y) KS_INLINE {
+    const Wide w = whole(scaled_weight(r, s.table, y));
+    return r.best - y > r.reach ? 0ull : w;
+  };
 
   // ---- cuts ----
   bool counted = false;  // the histogram over all candidates is there, over the cluster
   const int mine = kBins / ctas, per = (mine + kThreads - 1) / kThreads;  // bins of this CTA, and of a thread
   const unsigned* m_count = ctas == 1 ? s.count : s.m_count;
-  auto m_sum = [&](int i) { return ctas == 1 ? (static_cast<Wide>(s.high[i]) << 32) + s.low[i] : s.m_sum[i]; };
+  auto m_sum = [&](int i) KS_INLINE { return ctas == 1 ? (static_cast<Wide>(s.high[i]) << 32) + s.low[i] : s.m_sum[i]; };
   // histogram of the candidates that `digit` gives a bin (-1: none), and this CTA's share of it over the cluster
-  auto histogram = [&](bool clear, auto digit) {
+  auto histogram = [&](bool clear, auto digit) KS_INLINE {
     if (clear) {
       for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.low[i] = s.high[i] = 0;
       __syncthreads();
     }
-    each([&](int64_t i, float y) {
-      if (r.best - y > r.reach) return;
-      const Wide w = weight(y);
-      if (w == 0) return;
-      const int d = digit(i, y);
-      if (d < 0) return;
-      atomicAdd(&s.count[d], 1u);
-      // 64 bits in two additions of 32: who sees the low one wrap carries
-      const unsigned add = static_cast<unsigned>(w), was = atomicAdd(&s.low[d], add);
-      const unsigned up = static_cast<unsigned>(w >> 32) + (was + add < was ? 1u : 0u);
-      if (up) atomicAdd(&s.high[d], up);
+    each([&](int64_t i, const float (&y)[V]) KS_INLINE {
+      Wide w[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) w[v] = weight(y[v]);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int d = digit(i + v, y[v]);
+        if (w[v] == 0 || d < 0) continue;
+        atomicAdd(&s.count[d], 1u);
+        // 64 bits in two additions of 32: who sees the low one wrap carries
+        const unsigned add = static_cast<unsigned>(w[v]), was = atomicAdd(&s.low[d], add);
+        const unsigned up = static_cast<unsigned>(w[v] >> 32) + (was + add < was ? 1u : 0u);
+        if (up) atomicAdd(&s.high[d], up);
+      }
     });
     meet(ctas);
     Wide c = 0, w = 0;
@@ -375,10 +426,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   };
   // The front of `n` candidates (n > 0), or else the shortest whose weights sum to `part` of `of` (0: of all), as a cut; the
   // sum of its weights, 0 where nothing is cut.
-  auto find_cut = [&](Wide n, double part, Wide of) -> Wide {
+  auto find_cut = [&](Wide n, double part, Wide of) KS_INLINE -> Wide {
     const Wide outer = cut;  // what an earlier cut leaves
     if (!counted) {
-      histogram(false, [&](int64_t, float y) { return bin_of(r, y); });
+      histogram(false, [&](int64_t, float y) KS_INLINE { return bin_of(r, y); });
       counted = true;
     }
     Wide base_count = 0, base_sum = 0, prefix = 0;
@@ -444,21 +495,24 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       const int shift_now = 64 - kDigit * level;  // of the digits that are fixed
       if (level == 0) bin0 = bin;
       else prefix |= static_cast<Wide>(kBins - 1 - bin) << (shift_now > 0 ? shift_now : 0);
-      auto member = [&](Wide key, float y) {
+      auto member = [&](Wide key, float y) KS_INLINE {
         return bin_of(r, y) == bin0 && key >= outer && (level == 0 || (key >> (shift_now > 0 ? shift_now : 0)) == (prefix >> (shift_now > 0 ? shift_now : 0)));
       };
       if (held <= kList) {
         unsigned* n_list = of_rank(&s.listed, owner, ctas);
         Wide* list = of_rank(&s.list[0], owner, ctas);
-        each([&](int64_t i, float y) {
-          const Wide key = key_of(i, y);
-          if (!member(key, y) || r.best - y > r.reach || weight(y) == 0) return;
-          list[atomicAdd(n_list, 1u)] = key;
+        each([&](int64_t i, const float (&y)[V]) KS_INLINE {
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            if (bin_of(r, y[v]) != bin0) continue;
+            const Wide key = key_of(i + v, y[v]);
+            if (member(key, y[v]) && weight(y[v]) > 0) list[atomicAdd(n_list, 1u)] = key;
+          }
         });
         meet(ctas);
         if (rank == owner) {
           const int n_held = static_cast<int>(s.listed);
-          sort_list(s.list, n_held);
+          sort_list<kThreads>(s.list, n_held);
           constexpr int kEach = kList / kThreads;
           Wide w2[kEach], sum2 = 0, total;
 #pragma unroll
@@ -488,7 +542,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
       counted = false;
       const int next = shift_now - kDigit > 0 ? shift_now - kDigit : 0;
       const int width = shift_now - next;
-      histogram(true, [&](int64_t i, float y) {
+      histogram(true, [&](int64_t i, float y) KS_INLINE {
         const Wide key = key_of(i, y);
         if (!member(key, y)) return -1;
         return kBins - 1 - static_cast<int>((key >> next) & ((1u << width) - 1));
@@ -500,7 +554,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (set.top_p < 1.0f) {  // of what top-k leaves
       if (sum > 0 && !counted) {  // (narrowed down: the histogram is that of one bin)
         const Wide outer = cut;
-        histogram(true, [&](int64_t i, float y) { return key_of(i, y) >= outer ? bin_of(r, y) : -1; });
+        histogram(true, [&](int64_t i, float y) KS_INLINE { return key_of(i, y) >= outer ? bin_of(r, y) : -1; });
         counted = true;
       }
       find_cut(0, fmax(static_cast<double>(set.top_p), 0.0), sum);
@@ -510,20 +564,44 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
   // ---- the sum of what stays, then the draws, in the order of the indices ----
   const float cut_score = cut > 0 ? key_score(cut) : none;
   const unsigned cut_at = cut > 0 ? static_cast<unsigned>(key_index(cut)) : 0xFFFFFFFFu;
-  auto stays = [&](int64_t i, float y) -> Wide {
-    if (!(y > cut_score) && !(y == cut_score && y > none && static_cast<unsigned>(i - shift) <= cut_at)) return 0;
-    if (greedy) return 1;
-    if (r.best - y > r.reach) return 0;
+  auto stays = [&](int64_t i, float y) KS_INLINE -> Wide {
+    const bool in = y > cut_score || (y == cut_score && static_cast<unsigned>(i - shift) <= cut_at);
     const double w = scaled_weight(r, s.table, y);
-    return w >= r.least ? whole(w) : 0;
+    return in && !(r.best - y > r.reach) && (greedy || w >= r.least) ? (greedy ? 1ull : whole(w)) : 0ull;
   };
-  Wide sum = 0;
-  each([&](int64_t i, float y) { sum += stays(i, y); });
-  const Wide warp_total = warp_sum(sum);
-  Wide total;
-  Wide below = block_scan(lane == 0 ? warp_total : 0, s.warp, total);  // of the warps before
-  below = __shfl_sync(0xFFFFFFFFu, below, 0);
-  if (threadIdx.x == 0) s.total = total;
+  const int entries = tiles * kWarps;  // a tile's parts by warp, in the order of the indices
+  __syncthreads();  // (the list is read)
+  for (int tile = 0; tile < tiles; ++tile) {
+    Wide own = 0;
+    int64_t at = place(tile, warp, 0);
+    uint4 next = get(tile, warp, 0);
+#pragma unroll 1
+    for (int q = 0; q < loads && at - lane * V < last; ++q, at += 32 * V) {
+      float y[V];
+      unpack(next, y, T{});
+      if (q + 1 < loads) next = get(tile, warp, q + 1);
+      // (where a cut leaves nothing of a warp's scores there is nothing to compute)
+      float most = y[0];
+#pragma unroll
+      for (int v = 1; v < V; ++v) most = fmaxf(most, y[v]);
+      if (!__any_sync(0xFFFFFFFFu, most >= cut_score && most > none)) continue;
+#pragma unroll
+      for (int v = 0; v < V; ++v) own += stays(at + v, y[v]);
+    }
+    own = warp_sum(own);
+    if (lane == 0) s.list[tile * kWarps + warp] = own;
+  }
+  __syncthreads();
+  {  // sums up to an entry's end
+    const int per_thread = (entries + kThreads - 1) / kThreads;
+    Wide own = 0, total;
+    for (int e = 0; e < per_thread; ++e)
+      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) own += s.list[threadIdx.x * per_thread + e];
+    Wide upto = block_scan(own, s.warp, total);
+    for (int e = 0; e < per_thread; ++e)
+      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) s.list[threadIdx.x * per_thread + e] = upto += s.list[threadIdx.x * per_thread + e];
+    if (threadIdx.x == 0) s.total = total;
+  }
   meet(ctas);
   Wide all = 0, before = 0;
   for (int o = 0; o < ctas; ++o) {
@@ -531,94 +609,64 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const __grid_consta
     if (o < rank) before += t;
     all += t;
   }
-  // lane q has draw q
-  Wide at = ~0ull;
-  if (lane < a.draws) {
-    const float u = a.u[p * a.draws + lane];
-    at = static_cast<Wide>(static_cast<double>(u > 0.0f ? u : 0.0f) * static_cast<double>(all));
-    if (u >= 1.0f || at >= all) at = all - 1;
-  }
-  const double log_all = log(static_cast<double>(all) / (greedy ? 1.0 : r.one));
-  auto resolve = [&](int tile, Wide from, Wide to) {  // the draws that fall to this warp's scores of a tile
-    unsigned hits = __ballot_sync(0xFFFFFFFFu, at >= from && at < to);
-    while (hits) {
-      const int q_draw = __ffs(hits) - 1;
-      hits &= hits - 1;
-      const Wide target = __shfl_sync(0xFFFFFFFFu, at, q_draw);
-      Wide done = from;
-#pragma unroll 1
-      for (int q = 0; q < loads; ++q) {
-        const uint4 raw = get(tile, q);
-        const int64_t i0 = place(tile, q);
-        Wide w[V], own = 0;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          w[v] = stays(i0 + v, score(raw, v));
-          own += w[v];
-        }
-        const Wide in = warp_scan(own, lane), row_total = __shfl_sync(0xFFFFFFFFu, in, 31);
-        if (target < done + row_total) {
-          Wide lo = done + in - own;
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            if (target >= lo && target < lo + w[v]) {
-              const float y = score(raw, v);
-              a.idx[p * a.draws + q_draw] = static_cast<int32_t>(i0 + v - shift);
-              if (a.logp) {
-                const double d = y == r.best ? 0.0 : (static_cast<double>(y) - r.best_wide) / static_cast<double>(set.temperature);
-                a.logp[p * a.draws + q_draw] = static_cast<float>(d - log_all);
-              }
-            }
-            lo += w[v];
-          }
-          break;
-        }
-        done += row_total;
-      }
+  for (int q_draw = warp; q_draw < a.draws; q_draw += kWarps) {
+    const float u = a.u[p * a.draws + q_draw];
+    Wide target = static_cast<Wide>(static_cast<double>(u > 0.0f ? u : 0.0f) * static_cast<double>(all));
+    if (u >= 1.0f || target >= all) target = all - 1;
+    if (target < before || target - before >= s.total) continue;
+    target -= before;
+    int lo = 0, hi = entries - 1;  // the first entry whose end is behind the target
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (s.list[mid] > target) hi = mid;
+      else lo = mid + 1;
     }
-  };
-  if (tiles == 1) {
-    resolve(0, before + below, before + below + warp_total);
-  } else {
-    Wide from = before;
-    for (int tile = 0; tile < tiles; ++tile) {
-      Wide own = 0;
+    target -= lo > 0 ? s.list[lo - 1] : 0;
+    const int tile = lo / kWarps, w_slot = lo % kWarps;
 #pragma unroll 1
-      for (int q = 0; q < loads; ++q) {
-        const uint4 raw = fetch(place(tile, q));
+    for (int q = 0; q < loads; ++q) {
+      float y[V];
+      unpack(get(tile, w_slot, q), y, T{});
+      const int64_t i0 = place(tile, w_slot, q);
+      Wide w[V], own = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) own += stays(place(tile, q) + v, score(raw, v));
+      for (int v = 0; v < V; ++v) {
+        w[v] = stays(i0 + v, y[v]);
+        own += w[v];
       }
-      own = warp_sum(own);
-      Wide b = block_scan(lane == 0 ? own : 0, s.warp, total);
-      b = __shfl_sync(0xFFFFFFFFu, b, 0);
-      resolve(tile, from + b, from + b + own);
-      from += total;
+      const Wide row_total = warp_sum(own);
+      if (target >= row_total) {
+        target -= row_total;
+        continue;
+      }
+      Wide from = warp_scan(own, lane) - own;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (target >= from && target < from + w[v]) {
+          a.idx[p * a.draws + q_draw] = static_cast<int32_t>(i0 + v - shift);
+          if (a.logp) {
+            const double d = y[v] == r.best ? 0.0 : (static_cast<double>(y[v]) - r.best_wide) / static_cast<double>(set.temperature);
+            a.logp[p * a.draws + q_draw] = static_cast<float>(d - log(static_cast<double>(all) / (greedy ? 1.0 : r.one)));
+          }
+        }
+        from += w[v];
+      }
+      break;
     }
   }
   meet(ctas);  // (its sum is read by the others)
 }
 
-template <typename T>
-cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
-  constexpr int64_t kLoad = kThreads * (16 / sizeof(T));  // scores of one load of a CTA
-  const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
-  int ctas = 1;
-  while (ctas < kMaxCtas && kLoad * kLoads * ctas < len) ctas *= 2;
-  // few rows: more CTAs each, while they have a thousand scores and more
-  while (ctas < kMaxCtas && a.p * ctas * 2 <= 148 && len / (2 * ctas) >= 1024) ctas *= 2;
-  // (a stretch is rounded up to whole warps' loads and may begin within one)
-  const int64_t each = (len + ctas - 1) / ctas + 64 * (16 / sizeof(T));
-  const int loads = static_cast<int>(std::min<int64_t>(kLoads, (each + kLoad - 1) / kLoad));
-  if (a.p * ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
-  const void* kernel = reinterpret_cast<const void*>(&sample_kernel<T>);
-  cudaError_t e = ensure_dynamic_smem(kernel, kLoads * kThreads * 16);
+template <typename T, int kThreads>
+cudaError_t launch_as(const SampleArgs& a, int ctas, int held_loads, cudaStream_t stream) {
+  const void* kernel = reinterpret_cast<const void*>(&sample_kernel<T, kThreads>);
+  cudaError_t e = ensure_dynamic_smem(kernel, kHeldLoads * kThreads * 16);
   if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(a.p * ctas));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(loads) * kThreads * 16;
+  cfg.dynamicSmemBytes = static_cast<size_t>(held_loads) * kThreads * 16;
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -626,7 +674,29 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a, ctas, loads);
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads>, a, ctas, held_loads);
+}
+
+constexpr int kManyThreads = 256, kFewThreads = 512;
+constexpr int64_t kManyRows = 296;
+
+template <typename T>
+cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
+  constexpr int64_t kV = 16 / sizeof(T);
+  const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
+  // (a stretch is rounded up to whole warps' loads and may begin within one; four CTAs an SM keep 28 KB each)
+  if (a.p >= kManyRows) {
+    const int64_t loads = (2 * len + 64 * kV + kManyThreads * kV - 1) / (kManyThreads * kV);
+    return launch_as<T, kManyThreads>(a, 1, static_cast<int>(len > 7 * kManyThreads * kV ? 0 : std::min<int64_t>(7, loads)), stream);
+  }
+  int ctas = 1;
+  while (ctas < kMaxCtas && kFewThreads * kV * kHeldLoads * ctas < len) ctas *= 2;
+  // few rows: more CTAs each, while they have a thousand scores and more
+  while (ctas < kMaxCtas && a.p * ctas * 2 <= 148 && len / (2 * ctas) >= 1024) ctas *= 2;
+  if (a.p * ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+  const int64_t each = (a.seg_off ? 2 * len : len + ctas - 1) / ctas + 64 * kV;
+  const int64_t loads = std::min<int64_t>(kHeldLoads, (each + kFewThreads * kV - 1) / (kFewThreads * kV));
+  return launch_as<T, kFewThreads>(a, ctas, static_cast<int>(loads), stream);
 }
 
 }  // namespace
