@@ -15,6 +15,7 @@
 // longer ones (1,024 x 60,000 scores: 947 us by clusters of 4).
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "ks_e4m3.cuh"
 #include "ks_internal.h"
@@ -38,6 +39,7 @@ constexpr int kMaxCtas = 16;       // of a cluster
 constexpr int kHeldLoads = 8;      // 16-byte loads that a thread keeps at most
 constexpr int kEntries = 1024;     // sums over stretches of a row that a CTA keeps
 constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (51 bits)
+constexpr int kTable = 256;        // powers of two within one octave
 constexpr int kDigit = 10;         // bits of (score, index) that a bin is narrowed down by
 
 struct Row {
@@ -45,27 +47,26 @@ struct Row {
   float reach;        // scores further below the best one have no weight
   float bins;         // bins a unit of score
   double best_wide;
-  double steps;       // 64ths of a power of two a unit of score
+  double steps;       // 256ths of a power of two a unit of score
   double one;         // weight of the best score, 2^s
   double least;       // weights below do not stay (min-p)
 };
 
-// Weight of a score within reach in units of 2^-s, before it is rounded: 2^(n / 64) from a table of 64 (times 2^s) and the
-// exponent, times the exponential of what is left, at most ln 2 / 128, by its series (P. T. P. Tang's table-driven method, ACM
+// Weight of a score within reach in units of 2^-s, before it is rounded: 2^(n / 256) from a table of 256 (times 2^s) and the
+// exponent, times the exponential of what is left, at most ln 2 / 512, by its series (P. T. P. Tang's table-driven method, ACM
 // TOMS 15, 1989). The first term that is left out is below 2^-54. The best score's weight is exact, also where it is infinite.
 __device__ __forceinline__ double scaled_weight(const Row& r, const double* table, float x) {
   constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to a whole number in the low word
-  constexpr double kL = 0.69314718055994530942 / 64.0;
+  constexpr double kL = 0.69314718055994530942 / kTable;
   const double z = (static_cast<double>(x) - r.best_wide) * r.steps, m = z + kRound;
   const int n = __double2loint(m);
   const double f = z - (m - kRound);
-  double e = fma(f, kL * kL * kL * kL * kL / 120.0, kL * kL * kL * kL / 24.0);
-  e = fma(f, e, kL * kL * kL / 6.0);
+  double e = fma(f, kL * kL * kL * kL / 24.0, kL * kL * kL / 6.0);
   e = fma(f, e, kL * kL / 2.0);
   e = fma(f, e, kL);
   e = fma(f, e, 1.0);
-  const double w = table[n & 63] * e;
-  const double v = __hiloint2double(__double2hiint(w) + ((n >> 6) << 20), __double2loint(w));
+  const double w = table[n & (kTable - 1)] * e;
+  const double v = __hiloint2double(__double2hiint(w) + ((n >> 8) << 20), __double2loint(w));
   return x == r.best ? r.one : v;
 }
 // rounded; w <= 2^51, so that the sum's low bits are the whole number
@@ -105,41 +106,19 @@ __device__ __forceinline__ Wide block_scan(Wide v, Wide (&s_warp)[kWarps], Wide&
   return (warp > 0 ? before : 0) + in - v;
 }
 
-// The same of two numbers at once.
-template <int kWarps>
-__device__ __forceinline__ void block_scan2(Wide& v, Wide& w, Wide (&s_warp)[2][kWarps], Wide& total_v, Wide& total_w) {
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const Wide in_v = warp_scan(v, lane), in_w = warp_scan(w, lane);
-  __syncthreads();
-  if (lane == 31) {
-    s_warp[0][warp] = in_v;
-    s_warp[1][warp] = in_w;
-  }
-  __syncthreads();
-  const Wide all_v = warp_scan(lane < kWarps ? s_warp[0][lane] : 0, lane), all_w = warp_scan(lane < kWarps ? s_warp[1][lane] : 0, lane);
-  total_v = __shfl_sync(0xFFFFFFFFu, all_v, kWarps - 1);
-  total_w = __shfl_sync(0xFFFFFFFFu, all_w, kWarps - 1);
-  const Wide before_v = __shfl_sync(0xFFFFFFFFu, all_v, warp > 0 ? warp - 1 : 0);
-  const Wide before_w = __shfl_sync(0xFFFFFFFFu, all_w, warp > 0 ? warp - 1 : 0);
-  v = (warp > 0 ? before_v : 0) + in_v - v;
-  w = (warp > 0 ? before_w : 0) + in_w - w;
-}
-
 template <int kWarps>
 struct Shared {
-  double table[64];
-  unsigned count[kBins];
-  unsigned low[kBins], high[kBins];  // of a bin's sum
-  unsigned m_count[kBins / 2];  // this CTA's share of the bins, over the cluster
-  Wide m_sum[kBins / 2];
+  double table[kTable];
+  unsigned low[kBins], high[kBins];  // of a bin's count or sum
+  Wide merged[kBins / 2];            // this CTA's share of the bins, over the cluster
   Wide list[kList];
-  Wide warp[kWarps], warp2[2][kWarps];
+  Wide warp[kWarps];
   // what the cluster's other CTAs read
   Wide best;
   float least[kWarps], min;
-  Wide share_count, share_sum, before_count, before_sum, total, cut, cut_sum;
+  Wide share, before, total, cut;
   int bin;
-  unsigned held, listed;
+  unsigned listed;
 };
 
 template <typename U>
@@ -202,13 +181,24 @@ __device__ __forceinline__ void unpack(const uint4& w, float (&y)[8], __half) {
     y[2 * i + 1] = normal(f.y);
   }
 }
-// Four bytes of a load: scores where `live` says so, -inf elsewhere.
-__device__ __forceinline__ uint32_t word_of(const float* base, bool live) { return live ? __float_as_uint(*base) : 0xFF800000u; }
+// The load of scores at a place of which some lie outside [shift, last): those as -inf.
 template <typename T>
-__device__ __forceinline__ uint32_t word_of(const T* base, bool live0, bool live1, uint32_t none) {
-  const uint32_t lo = live0 ? *reinterpret_cast<const uint16_t*>(base) : none;
-  const uint32_t hi = live1 ? *reinterpret_cast<const uint16_t*>(base + 1) : none;
-  return lo | (hi << 16);
+__device__ __noinline__ uint4 fetch_edge(const T* base, uint32_t at, uint32_t shift, uint32_t last) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      const uint32_t e = at + i;
+      u[i] = e >= shift && e < last ? __float_as_uint(base[e]) : 0xFF800000u;
+    } else {
+      constexpr uint32_t kNone = is_bf16<T> ? 0xFF80u : 0xFC00u;
+      const uint32_t e = at + 2 * i;
+      const uint32_t lo = e >= shift && e < last ? *reinterpret_cast<const uint16_t*>(base + e) : kNone;
+      const uint32_t hi = e + 1 >= shift && e + 1 < last ? *reinterpret_cast<const uint16_t*>(base + e + 1) : kNone;
+      u[i] = lo | (hi << 16);
+    }
+  }
+  return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
 template <typename T, int kThreads>
@@ -231,43 +221,42 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   // sums over their warps' parts to be kept.
   const int shift = static_cast<int>(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
   const T* base = row - shift;
-  const int64_t places = static_cast<int64_t>(len) + shift;
-  const int64_t chunk = ((places + ctas - 1) / ctas + 32 * V - 1) / (32 * V) * (32 * V);
-  const int64_t first = rank * chunk, last = first + chunk < places ? first + chunk : places;
-  const int64_t all_loads = first < last ? (last - first + kThreads * V - 1) / (kThreads * V) : 0;
-  const bool held = all_loads <= held_loads;
-  const int64_t least_loads = (all_loads + kEntries / kWarps - 1) / (kEntries / kWarps);
+  // (a row has less than 2^31 scores: places fit 32 bits)
+  const uint32_t places = static_cast<uint32_t>(len) + shift;
+  const uint32_t chunk = (places / ctas + 32 * V) / (32 * V) * (32 * V);
+  const uint64_t begin_at = static_cast<uint64_t>(rank) * chunk;
+  const uint32_t first = begin_at < places ? static_cast<uint32_t>(begin_at) : places;
+  const uint32_t last = chunk < places - first ? first + chunk : places;
+  const uint32_t all_loads = (last - first + kThreads * V - 1) / (kThreads * V);
+  const bool held = all_loads <= static_cast<uint32_t>(held_loads);
+  const uint32_t least_loads = (all_loads + kEntries / kWarps - 1) / (kEntries / kWarps);
   const int loads = static_cast<int>(held ? all_loads : least_loads > kHeldLoads ? least_loads : kHeldLoads);
   const int tiles = loads > 0 ? static_cast<int>((all_loads + loads - 1) / loads) : 0;
+  // loads at places from `shift` to here lie inside
+  const uint32_t inner = last >= static_cast<uint32_t>(shift) + V ? last - shift - V + 1 : 0;
 
-  auto fetch = [&](int64_t at) KS_INLINE {  // the load of V scores at a place; what lies outside the stretch as -inf
-    if (at >= shift && at + V <= last) return __ldg(reinterpret_cast<const uint4*>(base + at));
-    uint32_t u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t e = at + i * (V / 4);
-      const bool live0 = e >= shift && e < last, live1 = e + 1 >= shift && e + 1 < last;
-      if constexpr (V == 4) u[i] = word_of(reinterpret_cast<const float*>(base + e), live0);
-      else u[i] = word_of(base + e, live0, live1, sizeof(T) == 2 && is_bf16<T> ? 0xFF80u : 0xFC00u);
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
+  auto fetch = [&](uint32_t at) KS_INLINE {
+    return at - shift < inner ? __ldg(reinterpret_cast<const uint4*>(base + at)) : fetch_edge(base, at, shift, last);
   };
   // Place of a load: those of a warp are neighbours, and warps follow one another in a tile.
   auto place = [&](int tile, int w, int q) KS_INLINE {
-    return first + ((static_cast<int64_t>(tile) * kWarps + w) * loads + q) * (32 * V) + lane * V;
+    return first + ((static_cast<uint32_t>(tile) * kWarps + w) * loads + q) * (32 * V) + lane * V;
   };
-  auto get = [&](int tile, int w, int q) KS_INLINE { return held ? s_held[q * kThreads + w * 32 + lane] : fetch(place(tile, w, q)); };
-  auto key_of = [&](int64_t at, float y) KS_INLINE { return make_key(y, static_cast<int>(at - shift)); };
+  auto get = [&](uint32_t at, int w, int q) KS_INLINE { return held ? s_held[q * kThreads + w * 32 + lane] : fetch(at); };
+  auto key_of = [&](uint32_t at, float y) KS_INLINE { return make_key(y, static_cast<int>(at - shift)); };
   // f(place, scores) for all loads of this thread
   auto each = [&](auto f) KS_INLINE {
     for (int tile = 0; tile < tiles; ++tile) {
-      int64_t at = place(tile, warp, 0);
-      uint4 next = get(tile, warp, 0);
+      uint32_t at = place(tile, warp, 0);
+      const uint32_t lane0 = at - lane * V;
+      if (lane0 >= last) break;
+      const int mine = min(loads, static_cast<int>((last - lane0 + 32 * V - 1) / (32 * V)));
+      uint4 next = get(at, warp, 0);
 #pragma unroll 1
-      for (int q = 0; q < loads && at - lane * V < last; ++q, at += 32 * V) {
+      for (int q = 0; q < mine; ++q, at += 32 * V) {
         float y[V];
         unpack(next, y, T{});
-        if (q + 1 < loads) next = get(tile, warp, q + 1);  // on its way while these are worked on
+        if (q + 1 < mine) next = get(at + 32 * V, warp, q + 1);  // on its way while these are worked on
         f(at, y);
       }
     }
@@ -277,10 +266,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   float top = none, low = __int_as_float(0x7F800000);
   for (int tile = 0; tile < tiles; ++tile)
     for (int q0 = 0; q0 < loads; q0 += 4) {
+      const uint32_t at = place(tile, warp, q0);
       uint4 w[4];
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (q0 + q < loads) w[q] = fetch(place(tile, warp, q0 + q));
+        if (q0 + q < loads) w[q] = fetch(at + q * (32 * V));
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         if (q0 + q >= loads) break;
@@ -299,10 +289,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   Wide best = top > none ? make_key(top, 0) : 0;
   if (greedy && top > none) {
     unsigned at = 0xFFFFFFFFu;
-    each([&](int64_t i, const float (&y)[V]) KS_INLINE {
+    each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (y[v] == top) at = min(at, static_cast<unsigned>(i + v - shift));
+        if (y[v] == top) at = min(at, i + v - shift);
     });
     best = make_key(top, static_cast<int>(at));
   }
@@ -332,7 +322,6 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
       s.listed = 0;
     }
   }
-  for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.low[i] = s.high[i] = 0;
   meet(ctas);
   best = 0;
   for (int r = 0; r < ctas; ++r) {
@@ -353,17 +342,21 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   Row r;
   r.best = key_score(best);
   r.best_wide = static_cast<double>(r.best);
-  r.steps = greedy ? 0.0 : 64.0 * 1.4426950408889634074 / static_cast<double>(set.temperature);
+  r.steps = greedy ? 0.0 : kTable * 1.4426950408889634074 / static_cast<double>(set.temperature);
   r.one = ldexp(1.0, min(51, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
   r.least = set.min_p > 0.0f ? fmin(static_cast<double>(set.min_p), 1.0) * r.one : 0.0;
   r.reach = greedy ? 0.0f : (kReach + 1.0f) * set.temperature;
   // bins over what the scores reach, but no further than weights do
   const float span = fminf(r.best - low, kReach * set.temperature);
   r.bins = span > 0.0f ? static_cast<float>(kBins - 1) / span : 0.0f;
-  if (threadIdx.x < 64) s.table[threadIdx.x] = exp2(threadIdx.x / 64.0) * r.one;
+  if (threadIdx.x < kTable) s.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / kTable) * r.one;
   __syncthreads();
-  // what stays: scores above `cut_score`, and those that equal it up to the place `cut_at`
-  Wide cut = greedy ? best : 0;
+  // what stays: scores above `cut_score`, and of those that equal it the ones up to `cut_at`
+  float cut_score = greedy ? r.best : none;
+  unsigned cut_at = greedy ? static_cast<unsigned>(key_index(best)) : 0xFFFFFFFFu;
+  auto inside = [&](uint32_t i, float y) KS_INLINE {
+    return y > cut_score || (y == cut_score && i - shift <= cut_at);
+  };
   // (without a branch: what lies behind the reach of weights, -inf above all, computes something and gets 0)
   auto weight = [&](float y) KS_INLINE {
     const Wide w = whole(scaled_weight(r, s.table, y));
@@ -371,215 +364,183 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   };
 
   // ---- cuts ----
-  bool counted = false;  // the histogram over all candidates is there, over the cluster
   const int mine = kBins / ctas, per = (mine + kThreads - 1) / kThreads;  // bins of this CTA, and of a thread
-  const unsigned* m_count = ctas == 1 ? s.count : s.m_count;
-  auto m_sum = [&](int i) KS_INLINE { return ctas == 1 ? (static_cast<Wide>(s.high[i]) << 32) + s.low[i] : s.m_sum[i]; };
-  // histogram of the candidates that `digit` gives a bin (-1: none), and this CTA's share of it over the cluster
-  auto histogram = [&](bool clear, auto digit) KS_INLINE {
-    if (clear) {
-      for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = s.low[i] = s.high[i] = 0;
-      __syncthreads();
-    }
-    each([&](int64_t i, const float (&y)[V]) KS_INLINE {
-      Wide w[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) w[v] = weight(y[v]);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int d = digit(i + v, y[v]);
-        if (w[v] == 0 || d < 0) continue;
-        atomicAdd(&s.count[d], 1u);
-        // 64 bits in two additions of 32: who sees the low one wrap carries
-        const unsigned add = static_cast<unsigned>(w[v]), was = atomicAdd(&s.low[d], add);
-        const unsigned up = static_cast<unsigned>(w[v] >> 32) + (was + add < was ? 1u : 0u);
-        if (up) atomicAdd(&s.high[d], up);
-      }
-    });
-    meet(ctas);
-    Wide c = 0, w = 0;
-    if (ctas > 1)
-      for (int i = threadIdx.x; i < mine; i += kThreads) {
-        unsigned bc = 0;
-        Wide bw = 0;
-        for (int o = 0; o < ctas; ++o) {
-          bc += *of_rank(&s.count[rank * mine + i], o, ctas);
-          bw += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
-        }
-        s.m_count[i] = bc;
-        s.m_sum[i] = bw;
-        c += bc;
-        w += bw;
-      }
-    else
-      for (int i = threadIdx.x; i < mine; i += kThreads) {
-        c += m_count[i];
-        w += m_sum(i);
-      }
-    Wide total_c, total_w;
-    block_scan2(c, w, s.warp2, total_c, total_w);
-    if (threadIdx.x == 0) {
-      s.share_count = total_c;
-      s.share_sum = total_w;
-    }
-    meet(ctas);
-  };
-  // The front of `n` candidates (n > 0), or else the shortest whose weights sum to `part` of `of` (0: of all), as a cut; the
-  // sum of its weights, 0 where nothing is cut.
-  auto find_cut = [&](Wide n, double part, Wide of) KS_INLINE -> Wide {
-    const Wide outer = cut;  // what an earlier cut leaves
-    if (!counted) {
-      histogram(false, [&](int64_t, float y) KS_INLINE { return bin_of(r, y); });
-      counted = true;
-    }
-    Wide base_count = 0, base_sum = 0, prefix = 0;
-    int bin0 = 0, owner = 0;
-    double target = 0.0;
+  auto bin_sum = [&](int i) KS_INLINE { return ctas == 1 ? (static_cast<Wide>(s.high[i]) << 32) + s.low[i] : s.merged[i]; };
+  // Leaves the shortest front of what stays that holds `part` of its candidates' sum, or (`counts`) `n` candidates; the cut is
+  // the first candidate in the order up to which the bins, then the sorted ones of a bin, reach that.
+  auto find_cut = [&](auto counts, Wide n, double part) KS_INLINE {
+    constexpr bool kCounts = decltype(counts)::value;
+    Wide before = 0, target = n, prefix = 0;
+    int bin0 = 0;
     for (int level = 0;; ++level) {
+      const int fixed = level == 0 ? 64 : max(0, 64 - kDigit * (level - 1));  // bits of (score, index) above are `prefix`'s
+      const int next = max(0, fixed - kDigit);
+      auto member = [&](Wide key, float y) KS_INLINE {
+        return level == 0 || (bin_of(r, y) == bin0 && (level == 1 || (key >> fixed) == (prefix >> fixed)));
+      };
+      for (int i = threadIdx.x; i < kBins; i += kThreads) s.low[i] = s.high[i] = 0;
+      if (threadIdx.x == 0) s.listed = 0;
+      __syncthreads();
+      each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
+        bool in[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[v] = y[v] > none;
+        if (cut_score > none) {  // (where an earlier cut leaves nothing of a warp's scores there is nothing to compute)
+          bool any = false;
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            in[v] = inside(i + v, y[v]);
+            any = any || in[v];
+          }
+          if (!__any_sync(0xFFFFFFFFu, any)) return;
+        }
+        Wide w[V];
+        int bin[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          w[v] = kCounts ? 1ull : weight(y[v]);
+          bin[v] = bin_of(r, y[v]);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          if (!in[v]) continue;
+          int d = bin[v];
+          if (level > 0) {
+            const Wide key = key_of(i + v, y[v]);
+            if (!member(key, y[v])) continue;
+            d = kBins - 1 - static_cast<int>((key >> next) & ((1u << (fixed - next)) - 1));
+          }
+          // 64 bits in two additions of 32: who sees the low one wrap carries
+          const unsigned add = static_cast<unsigned>(w[v]), was = atomicAdd(&s.low[d], add);
+          if (!kCounts) {
+            const unsigned up = static_cast<unsigned>(w[v] >> 32) + (was + add < was ? 1u : 0u);
+            if (up) atomicAdd(&s.high[d], up);
+          }
+        }
+      });
+      meet(ctas);
+      Wide own = 0, share;
+      for (int i = threadIdx.x; i < mine; i += kThreads) {
+        Wide b = 0;
+        if (ctas == 1) {
+          b = bin_sum(i);
+        } else {
+          for (int o = 0; o < ctas; ++o)
+            b += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
+          s.merged[i] = b;
+        }
+        own += b;
+      }
+      block_scan(own, s.warp, share);
+      if (threadIdx.x == 0) s.share = share;
+      meet(ctas);
       // the CTA whose share of the bins holds the last candidate that stays
-      Wide c = base_count, w = base_sum, own_c = 0, own_w = 0, all_c = 0, all_w = 0;
+      Wide reached = before, own_before = before;
+      int owner = -1;
       for (int o = 0; o < ctas; ++o) {
-        all_c += *of_rank(&s.share_count, o, ctas);
-        all_w += *of_rank(&s.share_sum, o, ctas);
+        const Wide next_share = *of_rank(&s.share, o, ctas);
+        if (level == 0) own_before += next_share;  // (the sum of all)
       }
       if (level == 0) {
-        target = fmax(part * static_cast<double>(of > 0 ? of : all_w), 1.0);  // (weights are whole numbers: the best one stays)
-        if (n > 0 ? all_c <= n : static_cast<double>(of > 0 ? of : all_w) <= target) {
+        const Wide all = own_before;
+        if (!kCounts) target = max(1ull, static_cast<Wide>(ceil(part * static_cast<double>(all))));
+        if (all <= target) {
           meet(ctas);
-          return 0;
+          return;
         }
       }
-      owner = ctas - 1;
-      for (int o = 0; o < ctas; ++o) {
-        own_c = c;
-        own_w = w;
-        c += *of_rank(&s.share_count, o, ctas);
-        w += *of_rank(&s.share_sum, o, ctas);
-        if (n > 0 ? c >= n : static_cast<double>(w) >= target) {
-          owner = o;
-          break;
-        }
+      for (int o = 0; o < ctas && owner < 0; ++o) {
+        own_before = reached;
+        reached += *of_rank(&s.share, o, ctas);
+        if (reached >= target) owner = o;
       }
       if (rank == owner) {
-        Wide bc = 0, bw = 0, total_c, total_w;
-        for (int q = 0; q < per; ++q) {
+        Wide mine_sum = 0, total;
+        for (int q = 0; q < per; ++q)
+          if (static_cast<int>(threadIdx.x) * per + q < mine) mine_sum += bin_sum(threadIdx.x * per + q);
+        Wide b = block_scan(mine_sum, s.warp, total) + own_before;
+        for (int q = 0; q < per && static_cast<int>(threadIdx.x) * per + q < mine; ++q) {
           const int i = threadIdx.x * per + q;
-          if (i < mine) {
-            bc += m_count[i];
-            bw += m_sum(i);
-          }
-        }
-        block_scan2(bc, bw, s.warp2, total_c, total_w);
-        bc += own_c;
-        bw += own_w;
-        for (int q = 0; q < per; ++q) {
-          const int i = threadIdx.x * per + q;
-          if (i >= mine) break;
-          const bool starts = n > 0 ? bc < n : static_cast<double>(bw) < target;
-          const bool ends = n > 0 ? bc + m_count[i] >= n : static_cast<double>(bw + m_sum(i)) >= target;
-          if (m_count[i] > 0 && starts && ends) {
+          const Wide e = b + bin_sum(i);
+          if (b < target && e >= target) {
             s.bin = rank * mine + i;
-            s.held = m_count[i];
-            s.before_count = bc;
-            s.before_sum = bw;
+            s.before = b;
           }
-          bc += m_count[i];
-          bw += m_sum(i);
+          b = e;
         }
       }
       meet(ctas);
       const int bin = *of_rank(&s.bin, owner, ctas);
-      const unsigned held = *of_rank(&s.held, owner, ctas);
-      base_count = *of_rank(&s.before_count, owner, ctas);
-      base_sum = *of_rank(&s.before_sum, owner, ctas);
-      const int shift_now = 64 - kDigit * level;  // of the digits that are fixed
+      before = *of_rank(&s.before, owner, ctas);
       if (level == 0) bin0 = bin;
-      else prefix |= static_cast<Wide>(kBins - 1 - bin) << (shift_now > 0 ? shift_now : 0);
-      auto member = [&](Wide key, float y) KS_INLINE {
-        return bin_of(r, y) == bin0 && key >= outer && (level == 0 || (key >> (shift_now > 0 ? shift_now : 0)) == (prefix >> (shift_now > 0 ? shift_now : 0)));
-      };
-      if (held <= kList) {
-        unsigned* n_list = of_rank(&s.listed, owner, ctas);
-        Wide* list = of_rank(&s.list[0], owner, ctas);
-        each([&](int64_t i, const float (&y)[V]) KS_INLINE {
+      else prefix |= static_cast<Wide>(kBins - 1 - bin) << next;
+      // the bin's candidates, if they are few enough to be sorted
+      const int fixed_now = level == 0 ? 64 : next;
+      unsigned* n_list = of_rank(&s.listed, owner, ctas);
+      Wide* list = of_rank(&s.list[0], owner, ctas);
+      each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            if (bin_of(r, y[v]) != bin0) continue;
-            const Wide key = key_of(i + v, y[v]);
-            if (member(key, y[v]) && weight(y[v]) > 0) list[atomicAdd(n_list, 1u)] = key;
-          }
-        });
-        meet(ctas);
-        if (rank == owner) {
-          const int n_held = static_cast<int>(s.listed);
-          sort_list<kThreads>(s.list, n_held);
-          constexpr int kEach = kList / kThreads;
-          Wide w2[kEach], sum2 = 0, total;
-#pragma unroll
-          for (int q = 0; q < kEach; ++q) {
-            const int i = threadIdx.x * kEach + q;
-            w2[q] = i < n_held ? weight(key_score(s.list[i])) : 0;
-            sum2 += w2[q];
-          }
-          Wide bw = block_scan(sum2, s.warp, total) + base_sum;
-#pragma unroll
-          for (int q = 0; q < kEach; ++q) {
-            const int i = threadIdx.x * kEach + q;
-            if (i < n_held && (n > 0 ? base_count + i + 1 == n
-                                     : static_cast<double>(bw) < target && (static_cast<double>(bw + w2[q]) >= target || i + 1 == n_held))) {
-              s.cut = s.list[i];
-              s.cut_sum = bw + w2[q];
-            }
-            bw += w2[q];
-          }
-          if (threadIdx.x == 0) s.listed = 0;
+        for (int v = 0; v < V; ++v) {
+          if (bin_of(r, y[v]) != bin0 || !(y[v] > none)) continue;
+          const Wide key = key_of(i + v, y[v]);
+          if (!inside(i + v, y[v]) || (level > 0 && (key >> fixed_now) != (prefix >> fixed_now))) continue;
+          if (!kCounts && weight(y[v]) == 0) continue;
+          const unsigned at = atomicAdd(n_list, 1u);
+          if (at < kList) list[at] = key;
         }
-        meet(ctas);
-        cut = *of_rank(&s.cut, owner, ctas);
-        return *of_rank(&s.cut_sum, owner, ctas);
-      }
-      // too many to sort: by the next bits of (score, index)
-      counted = false;
-      const int next = shift_now - kDigit > 0 ? shift_now - kDigit : 0;
-      const int width = shift_now - next;
-      histogram(true, [&](int64_t i, float y) KS_INLINE {
-        const Wide key = key_of(i, y);
-        if (!member(key, y)) return -1;
-        return kBins - 1 - static_cast<int>((key >> next) & ((1u << width) - 1));
       });
+      meet(ctas);
+      const unsigned listed = *n_list;
+      if (listed > kList) {  // too many: by the next bits of (score, index)
+        meet(ctas);  // (the number is read)
+        continue;
+      }
+      if (rank == owner) {
+        sort_list<kThreads>(s.list, static_cast<int>(listed));
+        constexpr int kEach = kList / kThreads;
+        Wide w[kEach], sum = 0, total;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+          const unsigned i = threadIdx.x * kEach + q;
+          w[q] = i >= listed ? 0 : kCounts ? 1 : weight(key_score(s.list[i]));
+          sum += w[q];
+        }
+        Wide b = block_scan(sum, s.warp, total) + before;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+          if (b < target && b + w[q] >= target) s.cut = s.list[threadIdx.x * kEach + q];
+          b += w[q];
+        }
+      }
+      meet(ctas);
+      const Wide cut = *of_rank(&s.cut, owner, ctas);
+      cut_score = key_score(cut);
+      cut_at = static_cast<unsigned>(key_index(cut));
+      return;
     }
   };
-  if (!greedy) {
-    const Wide sum = set.top_k > 0 ? find_cut(static_cast<Wide>(set.top_k), 1.0, 0) : 0;
-    if (set.top_p < 1.0f) {  // of what top-k leaves
-      if (sum > 0 && !counted) {  // (narrowed down: the histogram is that of one bin)
-        const Wide outer = cut;
-        histogram(true, [&](int64_t i, float y) KS_INLINE { return key_of(i, y) >= outer ? bin_of(r, y) : -1; });
-        counted = true;
-      }
-      find_cut(0, fmax(static_cast<double>(set.top_p), 0.0), sum);
-    }
-  }
+  if (!greedy && set.top_k > 0) find_cut(std::true_type{}, static_cast<Wide>(set.top_k), 0.0);
+  if (!greedy && set.top_p < 1.0f) find_cut(std::false_type{}, 0, fmax(static_cast<double>(set.top_p), 0.0));
 
   // ---- the sum of what stays, then the draws, in the order of the indices ----
-  const float cut_score = cut > 0 ? key_score(cut) : none;
-  const unsigned cut_at = cut > 0 ? static_cast<unsigned>(key_index(cut)) : 0xFFFFFFFFu;
-  auto stays = [&](int64_t i, float y) KS_INLINE -> Wide {
-    const bool in = y > cut_score || (y == cut_score && static_cast<unsigned>(i - shift) <= cut_at);
+  auto stays = [&](uint32_t i, float y) KS_INLINE -> Wide {
     const double w = scaled_weight(r, s.table, y);
-    return in && !(r.best - y > r.reach) && (greedy || w >= r.least) ? (greedy ? 1ull : whole(w)) : 0ull;
+    return inside(i, y) && !(r.best - y > r.reach) && (greedy || w >= r.least) ? (greedy ? 1ull : whole(w)) : 0ull;
   };
   const int entries = tiles * kWarps;  // a tile's parts by warp, in the order of the indices
   __syncthreads();  // (the list is read)
   for (int tile = 0; tile < tiles; ++tile) {
     Wide own = 0;
-    int64_t at = place(tile, warp, 0);
-    uint4 next = get(tile, warp, 0);
+    uint32_t at = place(tile, warp, 0);
+    const uint32_t lane0 = at - lane * V;
+    const int mine = lane0 >= last ? 0 : min(loads, static_cast<int>((last - lane0 + 32 * V - 1) / (32 * V)));
+    uint4 next = make_uint4(0, 0, 0, 0);
+    if (mine > 0) next = get(at, warp, 0);
 #pragma unroll 1
-    for (int q = 0; q < loads && at - lane * V < last; ++q, at += 32 * V) {
+    for (int q = 0; q < mine; ++q, at += 32 * V) {
       float y[V];
       unpack(next, y, T{});
-      if (q + 1 < loads) next = get(tile, warp, q + 1);
+      if (q + 1 < mine) next = get(at + 32 * V, warp, q + 1);
       // (where a cut leaves nothing of a warp's scores there is nothing to compute)
       float most = y[0];
 #pragma unroll
@@ -626,8 +587,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll 1
     for (int q = 0; q < loads; ++q) {
       float y[V];
-      unpack(get(tile, w_slot, q), y, T{});
-      const int64_t i0 = place(tile, w_slot, q);
+      const uint32_t i0 = place(tile, w_slot, q);
+      unpack(get(i0, w_slot, q), y, T{});
       Wide w[V], own = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
