@@ -34,6 +34,7 @@ KS_F32, KS_BF16, KS_F16, KS_E4M3 = range(4)
 KS_SCALE_F32, KS_SCALE_E8M0 = 0, 1
 KS_SCALE_BLOCK = 128
 _TYPES = {torch.float32: KS_F32, torch.bfloat16: KS_BF16, torch.float16: KS_F16, torch.float8_e4m3fn: KS_E4M3}
+_SCALE_TYPES = {torch.float32: KS_SCALE_F32, torch.float8_e8m0fnu: KS_SCALE_E8M0}
 _SCALES = {"f32": (KS_SCALE_F32, torch.float32), "e8m0": (KS_SCALE_E8M0, torch.float8_e8m0fnu)}
 SAMPLING_DT = np.dtype([("temperature", "<f4"), ("top_k", "<i4"), ("top_p", "<f4"), ("min_p", "<f4")])
 
@@ -138,19 +139,30 @@ def _dptr(t):
     return ctypes.c_void_p(t.data_ptr())
 
 
-def _rows(t, what):
+# The operators' small calls take a few microseconds on the device: their arguments go to the library as plain integers.
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _rows(t):
     """Pointer and row stride (elements) of a matrix whose rows may be padded."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: expected a CUDA matrix with contiguous rows")
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if not t.is_cuda or (cols > 1 and step != 1):
+        raise ValueError("expected a CUDA matrix with contiguous rows")
     # (torch gives a single row, or one of no columns, any stride)
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return ctypes.c_void_p(t.data_ptr()), ld
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
+
+
+def _flat(t):
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("expected a contiguous CUDA tensor")
+    return t.data_ptr()
 
 
 def _empty_e4m3(rows, cols, device):
     """[rows, cols] e4m3 whose rows begin on 16-byte boundaries."""
     wide = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
-    return wide[:, :cols]
+    return wide if cols % 16 == 0 else wide[:, :cols]
 
 
 def _hptr(a):
@@ -480,19 +492,21 @@ class Context:
         block_rows (1 or 128) x 128. Returns (q, scales); the rows of q begin on 16-byte boundaries."""
         rows, cols = x.shape
         st, dtype = _SCALES[scale]
-        br = max(int(block_rows), 1)  # an invalid one is reported by the library, not by torch
+        blocks = (-(-rows // max(int(block_rows), 1)), (cols + 127) // 128)  # an invalid one is reported by the library, not by torch
         if out is None:
             out = _empty_e4m3(rows, cols, self.device)
+        elif out.shape != x.shape or out.dtype != torch.float8_e4m3fn:
+            raise ValueError("quantize_e4m3: out")
         if out_scale is None:
-            out_scale = torch.empty(((rows + br - 1) // br, (cols + 127) // 128), dtype=dtype, device=self.device)
-        if x.dtype not in _TYPES or out.dtype != torch.float8_e4m3fn or out_scale.dtype != dtype:
-            raise ValueError("quantize_e4m3: element types")
-        if out.shape != x.shape or out_scale.shape != ((rows + br - 1) // br, (cols + 127) // 128):
-            raise ValueError("quantize_e4m3: shapes of the results")
-        xp, ldx = _rows(x, "x")
-        qp, ldq = _rows(out, "out")
-        self._check(_lib.ks_quantize_e4m3(self._h, xp, _TYPES[x.dtype], rows, cols, ldx, int(block_rows), st, qp,
-                                          ldq, _dptr(out_scale), _stream()), "ks_quantize_e4m3")
+            out_scale = torch.empty(blocks, dtype=dtype, device=self.device)
+        elif out_scale.shape != blocks or out_scale.dtype != dtype:
+            raise ValueError("quantize_e4m3: out_scale")
+        xp, ldx = _rows(x)
+        qp, ldq = _rows(out)
+        status = _lib.ks_quantize_e4m3(self._h, xp, _TYPES.get(x.dtype, -1), rows, cols, ldx, int(block_rows), st, qp, ldq,
+                                       _flat(out_scale), _raw_stream(self.device.index))
+        if status:
+            self._check(status, "ks_quantize_e4m3")
         return out, out_scale
 
     def matmul_e4m3(self, a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=torch.bfloat16, out=None,
@@ -501,28 +515,32 @@ class Context:
         Returns [m, n] of out_dtype; for torch.float8_e4m3fn (q, scales) with a scale for each row and 128 columns."""
         (m, k), (n, kb) = a.shape, b.shape
         blocks = (k + 127) // 128
-        if kb != k or a.dtype != torch.float8_e4m3fn or b.dtype != torch.float8_e4m3fn:
+        e4m3, scales = torch.float8_e4m3fn, a_scale.dtype
+        if kb != k or a.dtype != e4m3 or b.dtype != e4m3:
             raise ValueError("matmul_e4m3: operands")
-        if a_scale.dtype != b_scale.dtype or a_scale.dtype not in (torch.float32, torch.float8_e8m0fnu):
+        if scales not in _SCALE_TYPES or b_scale.dtype != scales:
             raise ValueError("matmul_e4m3: types of the scales")
         if a_scale.shape != (m, blocks) or b_scale.shape != ((n + 127) // 128, blocks):
             raise ValueError("matmul_e4m3: shapes of the scales")
         if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
             raise ValueError("matmul_e4m3: bias")
-        quantised = out_dtype == torch.float8_e4m3fn
+        quantised = out_dtype == e4m3
         if out is None:
             out = _empty_e4m3(m, n, self.device) if quantised else torch.empty((m, n), dtype=out_dtype, device=self.device)
+        elif out.shape != (m, n) or out.dtype != out_dtype:
+            raise ValueError("matmul_e4m3: out")
         if quantised and out_scale is None:
-            out_scale = torch.empty((m, (n + 127) // 128), dtype=a_scale.dtype, device=self.device)
-        if out.shape != (m, n) or out.dtype != out_dtype or out_dtype not in _TYPES or quantised != (out_scale is not None):
-            raise ValueError("matmul_e4m3: result")
-        if quantised and (out_scale.dtype != a_scale.dtype or out_scale.shape != (m, (n + 127) // 128)):
-            raise ValueError("matmul_e4m3: scales of the result")
-        (ap, lda), (bp, ldb), (op, ldd) = _rows(a, "a"), _rows(b, "b"), _rows(out, "out")
-        st = KS_SCALE_F32 if a_scale.dtype == torch.float32 else KS_SCALE_E8M0
-        self._check(_lib.ks_matmul_e4m3(self._h, ap, lda, _dptr(a_scale), bp, ldb, _dptr(b_scale), st, m, n, k,
-                                        _dptr(bias), int(relu), op, ldd, _TYPES[out_dtype], _dptr(out_scale), _stream()),
-                    "ks_matmul_e4m3")
+            out_scale = torch.empty((m, (n + 127) // 128), dtype=scales, device=self.device)
+        elif out_scale is not None and (not quantised or out_scale.dtype != scales or out_scale.shape != (m, (n + 127) // 128)):
+            raise ValueError("matmul_e4m3: out_scale")
+        ap, lda = _rows(a)
+        bp, ldb = _rows(b)
+        op, ldd = _rows(out)
+        status = _lib.ks_matmul_e4m3(self._h, ap, lda, _flat(a_scale), bp, ldb, _flat(b_scale), _SCALE_TYPES[scales], m, n, k,
+                                     None if bias is None else _flat(bias), int(relu), op, ldd, _TYPES.get(out_dtype, -1),
+                                     _flat(out_scale) if quantised else None, _raw_stream(self.device.index))
+        if status:
+            self._check(status, "ks_matmul_e4m3")
         return (out, out_scale) if quantised else out
 
     def sample(self, scores, u, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0,
@@ -536,22 +554,26 @@ class Context:
         if d_seg_off is None:
             if scores.shape[0] != P:
                 raise ValueError("sample: a row of scores for each row of u")
-            sp, ld = _rows(scores, "scores")
-            c = scores.shape[1]
+            sp, ld = _rows(scores)
+            c, off = scores.shape[1], None
         else:
             if d_seg_off.dtype != torch.int64 or d_seg_off.shape != (P + 1,):
                 raise ValueError("sample: d_seg_off")
-            sp, ld, c = _dptr(scores), 0, scores.numel()
+            sp, ld, c, off = _flat(scores), 0, scores.numel(), _flat(d_seg_off)
         if params is not None and params.numel() * params.element_size() != 16 * P:
             raise ValueError("sample: params")
         if out_idx is None:
             out_idx = torch.empty((P, draws), dtype=torch.int32, device=self.device)
             out_logp = torch.empty((P, draws), dtype=torch.float32, device=self.device)
-        if out_idx.shape != u.shape or (out_logp is not None and out_logp.shape != u.shape):
-            raise ValueError("sample: shapes of the results")
-        one = _Sampling(float(temperature), int(top_k), float(top_p), float(min_p))
-        self._check(_lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, _dptr(d_seg_off), ctypes.byref(one),
-                                   _dptr(params), _dptr(u), draws, _dptr(out_idx), _dptr(out_logp), _stream()), "ks_sample")
+        elif out_idx.shape != u.shape or out_idx.dtype != torch.int32 or (
+                out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32)):
+            raise ValueError("sample: out_idx, out_logp")
+        one = None if params is not None else ctypes.byref(_Sampling(temperature, top_k, top_p, min_p))
+        status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params),
+                                _flat(u), draws, _flat(out_idx), None if out_logp is None else _flat(out_logp),
+                                _raw_stream(self.device.index))
+        if status:
+            self._check(status, "ks_sample")
         return out_idx, out_logp
 
     # ---- search space and validity ----------------------------------------------------------

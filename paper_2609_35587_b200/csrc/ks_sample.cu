@@ -9,6 +9,9 @@
 // place in it. A histogram over the distance to the best score narrows it down to one bin, in which some hundred candidates
 // lie; they are sorted. Bins that hold more are narrowed down further by the bits of (score, index).
 //
+// A short front (top-k of some hundred) needs no histogram: the k-th largest of the maxima of 128 parts of the row bounds the
+// k-th score from below, so that little more than k candidates are listed, sorted, cut, and drawn from in the list.
+//
 // A row of a call with few rows belongs to a cluster of up to 16 CTAs that keep its scores in shared memory, each thread its
 // own; the CTAs' results meet there too. Where there are rows for the whole machine a CTA takes a row by itself and reads it
 // again in every phase, mostly from L2: four smaller CTAs an SM hide each other's barriers, of which a cluster has more and
@@ -36,6 +39,8 @@ template <> constexpr bool is_bf16<__nv_bfloat16> = true;
 constexpr int kBins = 1024;
 constexpr int kList = 1024;        // candidates of a bin that are sorted
 constexpr int kMaxCtas = 16;       // of a cluster
+constexpr int kParts = 128;        // of a CTA's scores, whose maxima bound a short front
+constexpr int kShort = 512, kShortParts = 112;  // the longest front that is drawn from a list, and its share of a CTA's parts
 constexpr int kHeldLoads = 8;      // 16-byte loads that a thread keeps at most
 constexpr int kEntries = 1024;     // sums over stretches of a row that a CTA keeps
 constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (51 bits)
@@ -109,13 +114,14 @@ __device__ __forceinline__ Wide block_scan(Wide v, Wide (&s_warp)[kWarps], Wide&
 template <int kWarps>
 struct Shared {
   double table[kTable];
-  unsigned low[kBins], high[kBins];  // of a bin's count or sum
+  alignas(16) unsigned low[kBins], high[kBins];  // of a bin's count or sum
   Wide merged[kBins / 2];            // this CTA's share of the bins, over the cluster
   Wide list[kList];
   Wide warp[kWarps];
   // what the cluster's other CTAs read
   Wide best;
-  float least[kWarps], min;
+  float least[kWarps], min, bound;
+  alignas(16) float part[kParts];
   Wide share, before, total, cut;
   int bin;
   unsigned listed;
@@ -302,11 +308,34 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     best = u > best ? u : best;
     low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, d));
   }
+  // the maxima of the parts, and the one that as many of them reach as the CTA's share of a short front has candidates
+  const int share = (set.top_k + ctas - 1) / ctas;
+  const bool short_front = !greedy && set.top_k > 0 && set.top_k <= kShort && share <= kShortParts;
+  if (short_front) {
+    constexpr int kEach = kThreads / kParts;
+    float most = top;
+#pragma unroll
+    for (int d = 1; d < kEach; d *= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, d));
+    if (threadIdx.x % kEach == 0) s.part[threadIdx.x / kEach] = most;
+  }
   if (lane == 0) {
     s.warp[warp] = best;
     s.least[warp] = low;
   }
   __syncthreads();
+  if (short_front && threadIdx.x < kParts) {
+    const float own = s.part[threadIdx.x];
+    int better = 0;
+#pragma unroll 8
+    for (int i = 0; i < kParts; i += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(&s.part[i]);
+      better += f.x > own || (f.x == own && i < static_cast<int>(threadIdx.x));
+      better += f.y > own || (f.y == own && i + 1 < static_cast<int>(threadIdx.x));
+      better += f.z > own || (f.z == own && i + 2 < static_cast<int>(threadIdx.x));
+      better += f.w > own || (f.w == own && i + 3 < static_cast<int>(threadIdx.x));
+    }
+    if (better == share - 1) s.bound = own;
+  }
   if (warp == 0) {
     best = lane < kWarps ? s.warp[lane] : 0;
     low = lane < kWarps ? s.least[lane] : low;
@@ -351,6 +380,96 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   r.bins = span > 0.0f ? static_cast<float>(kBins - 1) / span : 0.0f;
   if (threadIdx.x < kTable) s.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / kTable) * r.one;
   __syncthreads();
+  // ---- a short front ----
+  if (short_front) {
+    float bound = __int_as_float(0x7F800000);
+    for (int o = 0; o < ctas; ++o) bound = fminf(bound, *of_rank(&s.bound, o, ctas));
+    unsigned* n_list = of_rank(&s.listed, 0, ctas);
+    Wide* list = of_rank(&s.list[0], 0, ctas);
+    each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!(y[v] >= bound) || !(y[v] > none)) continue;
+        const unsigned at = atomicAdd(n_list, 1u);
+        if (at < kList) list[at] = key_of(i + v, y[v]);
+      }
+    });
+    meet(ctas);
+    const unsigned listed = *n_list;
+    if (listed <= kList) {
+      if (rank == 0) {
+        const int n = min(static_cast<int>(listed), set.top_k);
+        sort_list<kThreads>(s.list, static_cast<int>(listed));
+        constexpr int kEach = kShort / kThreads;
+        Wide w[kEach], sum = 0, all;
+        bool enough[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = threadIdx.x * kEach + e;
+          const float y = key_score(i < n ? s.list[i] : best);
+          const double exact = scaled_weight(r, s.table, y);
+          enough[e] = exact >= r.least;
+          w[e] = i < n && !(r.best - y > r.reach) ? whole(exact) : 0;
+          sum += w[e];
+        }
+        Wide b = block_scan(sum, s.warp, all);
+        const Wide target = set.top_p < 1.0f ? max(1ull, static_cast<Wide>(ceil(fmax(static_cast<double>(set.top_p), 0.0) * static_cast<double>(all)))) : all;
+        Wide place_of[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = threadIdx.x * kEach + e;
+          const bool in = w[e] > 0 && b < target && enough[e];
+          b += w[e];
+          if (i < kShort) s.merged[i] = in ? w[e] : 0;
+          place_of[e] = in ? ~((static_cast<Wide>(static_cast<unsigned>(key_index(s.list[i]))) << 32) | static_cast<unsigned>(i)) : 0;
+        }
+        // the weights that each candidate has, in the order of the indices
+        Wide* scores = reinterpret_cast<Wide*>(s.low);  // (kept by place in the sorted front)
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) scores[threadIdx.x * kEach + e] = threadIdx.x * kEach + e < n ? s.list[threadIdx.x * kEach + e] : 0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) s.list[threadIdx.x * kEach + e] = place_of[e];
+        __syncthreads();
+        sort_list<kThreads>(s.list, n);
+        sum = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = threadIdx.x * kEach + e;
+          const Wide key = i < n ? s.list[i] : 0;
+          w[e] = key > 0 ? s.merged[static_cast<unsigned>(~key)] : 0;
+          sum += w[e];
+        }
+        Wide upto = block_scan(sum, s.warp, all);
+        Wide* ends = reinterpret_cast<Wide*>(s.low) + kShort;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) ends[threadIdx.x * kEach + e] = upto += w[e];
+        __syncthreads();
+        for (int q = threadIdx.x; q < a.draws; q += kThreads) {
+          const float u = a.u[p * a.draws + q];
+          Wide goal = static_cast<Wide>(static_cast<double>(u > 0.0f ? u : 0.0f) * static_cast<double>(all));
+          if (u >= 1.0f || goal >= all) goal = all - 1;
+          int lo = 0, hi = n - 1;  // the first whose end is behind the goal
+          while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (ends[mid] > goal) hi = mid;
+            else lo = mid + 1;
+          }
+          const Wide key = scores[static_cast<unsigned>(~s.list[lo])];
+          const float y = key_score(key);
+          a.idx[p * a.draws + q] = key_index(key);
+          if (a.logp) {
+            const double d = y == r.best ? 0.0 : (static_cast<double>(y) - r.best_wide) / static_cast<double>(set.temperature);
+            a.logp[p * a.draws + q] = static_cast<float>(d - log(static_cast<double>(all) / r.one));
+          }
+        }
+      }
+      meet(ctas);  // (the number is read by the others)
+      return;
+    }
+    meet(ctas);  // (the number is read)
+  }
+
   // what stays: scores above `cut_score`, and of those that equal it the ones up to `cut_at`
   float cut_score = greedy ? r.best : none;
   unsigned cut_at = greedy ? static_cast<unsigned>(key_index(best)) : 0xFFFFFFFFu;
@@ -638,26 +757,28 @@ cudaError_t launch_as(const SampleArgs& a, int ctas, int held_loads, cudaStream_
   return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads>, a, ctas, held_loads);
 }
 
-constexpr int kManyThreads = 256, kFewThreads = 512;
+constexpr int kSmall = 256, kLarge = 512;  // threads of a CTA
 constexpr int64_t kManyRows = 296;
 
 template <typename T>
 cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
   constexpr int64_t kV = 16 / sizeof(T);
   const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
-  // (a stretch is rounded up to whole warps' loads and may begin within one; four CTAs an SM keep 28 KB each)
   if (a.p >= kManyRows) {
-    const int64_t loads = (2 * len + 64 * kV + kManyThreads * kV - 1) / (kManyThreads * kV);
-    return launch_as<T, kManyThreads>(a, 1, static_cast<int>(len > 7 * kManyThreads * kV ? 0 : std::min<int64_t>(7, loads)), stream);
+    // rows that four CTAs an SM keep (28 KB each; segments are of all lengths), else what is in work at a time stays in L2
+    constexpr int64_t kKept = 7;
+    if (len <= kKept * kSmall * kV)
+      return launch_as<T, kSmall>(a, 1, static_cast<int>(a.seg_off ? kKept : std::min(kKept, (len + 64 * kV) / (kSmall * kV) + 1)), stream);
+    return launch_as<T, kLarge>(a, 1, 0, stream);
   }
   int ctas = 1;
-  while (ctas < kMaxCtas && kFewThreads * kV * kHeldLoads * ctas < len) ctas *= 2;
+  while (ctas < kMaxCtas && kLarge * kV * kHeldLoads * ctas < len) ctas *= 2;
   // few rows: more CTAs each, while they have a thousand scores and more
   while (ctas < kMaxCtas && a.p * ctas * 2 <= 148 && len / (2 * ctas) >= 1024) ctas *= 2;
   if (a.p * ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
   const int64_t each = (a.seg_off ? 2 * len : len + ctas - 1) / ctas + 64 * kV;
-  const int64_t loads = std::min<int64_t>(kHeldLoads, (each + kFewThreads * kV - 1) / (kFewThreads * kV));
-  return launch_as<T, kFewThreads>(a, ctas, static_cast<int>(loads), stream);
+  const int64_t loads = std::min<int64_t>(kHeldLoads, (each + kLarge * kV - 1) / (kLarge * kV));
+  return launch_as<T, kLarge>(a, ctas, static_cast<int>(loads), stream);
 }
 
 }  // namespace
