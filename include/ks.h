@@ -186,6 +186,16 @@ ks_status ks_model_create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths,
                               const uint16_t* const* h_w_bf16, const float* const* h_bias,
                               const float* h_mu, const float* h_sigma, ks_model** out_model);
 
+/* Model B held in eight bits, with the same arguments (n_layers >= 2): the hidden layers' weights are quantised to e4m3 with a
+ * power of two as scale for each block of 128 x 128 (ks_quantize_e4m3 of the given bf16 weights, KS_SCALE_E8M0), and so are
+ * the rows that a layer reads, with a scale for each row and 128 of its values: the standardised inputs x' in fp32, and
+ * h = ReLU(W h_prev + b) of the fp32 sums of ks_matmul_e4m3. The last hidden layer is rounded to bf16 instead, and the last
+ * layer is s = w . h + b in fp32 as above. For the shapes that are bound by the tensor cores: ks_score and the ks_select calls
+ * serve it; ks_select holds at most 37,888 rows of activations at a time and 67 M scores. Synchronous. */
+ks_status ks_model_create_mlp_e4m3(ks_ctx* ctx, int n_layers, const int* h_widths,
+                                   const uint16_t* const* h_w_bf16, const float* const* h_bias,
+                                   const float* h_mu, const float* h_sigma, ks_model** out_model);
+
 /* The static sampling score of the paper's data-collection policy as a scorer with no learned
  * parameters: with n_c = ceil(M / (c_M T_M)) * ceil(N / (c_N T_N)) clusters and
  * W = ceil(n_c / S_SM) cluster waves, s = n_c / (W S_SM c_M c_N) * S * sqrt(T_M T_N T_K)

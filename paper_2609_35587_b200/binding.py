@@ -29,7 +29,8 @@ EXPORTS = ("ks_create", "ks_destroy", "ks_last_cuda_error", "ks_model_create_gbd
            "ks_select_one_prepared",
            "ks_debug_set_wait", "ks_debug_bounds_line", "ks_debug_bounds_clear", "ks_debug_walk_floor", "ks_debug_class_walks",
            "ks_debug_split_walks",
-           "ks_debug_limit_workspace", "ks_quantize_e4m3", "ks_matmul_e4m3", "ks_sample")
+           "ks_debug_limit_workspace", "ks_quantize_e4m3", "ks_matmul_e4m3", "ks_sample",
+           "ks_model_create_mlp_e4m3")
 KS_F32, KS_BF16, KS_F16, KS_E4M3 = range(4)
 KS_SCALE_F32, KS_SCALE_E8M0 = 0, 1
 KS_SCALE_BLOCK = 128
@@ -69,6 +70,7 @@ def _load() -> ctypes.CDLL:
     lib.ks_last_cuda_error.restype = ctypes.c_char_p
     lib.ks_model_create_gbdt.argtypes = [vp, i32, vp, vp, ctypes.c_float, ctypes.POINTER(vp)]
     lib.ks_model_create_mlp.argtypes = [vp, i32, vp, vp, vp, vp, vp, ctypes.POINTER(vp)]
+    lib.ks_model_create_mlp_e4m3.argtypes = lib.ks_model_create_mlp.argtypes
     lib.ks_model_create_static.argtypes = [vp, ctypes.POINTER(vp)]
     lib.ks_model_destroy.argtypes = [vp]
     lib.ks_featurize.argtypes = [vp, vp, i32, vp, i32, vp, vp, i64, vp, vp]
@@ -336,6 +338,13 @@ class Context:
         return Model(self, h, "gbdt", len(off) - 1)
 
     def model_create_mlp(self, mlp: dict) -> Model:
+        return self._model_create_mlp(mlp, "ks_model_create_mlp")
+
+    def model_create_mlp_e4m3(self, mlp: dict) -> Model:
+        """The same ranker with its hidden layers in eight bits (a scale for each block of 128)."""
+        return self._model_create_mlp(mlp, "ks_model_create_mlp_e4m3")
+
+    def _model_create_mlp(self, mlp: dict, name: str) -> Model:
         widths = np.ascontiguousarray(mlp["widths"], dtype=np.int32)
         L = len(widths) - 1
         ws = [np.ascontiguousarray(w, dtype=np.uint16) for w in mlp["weights"]]
@@ -345,10 +354,9 @@ class Context:
         wp = (ctypes.c_void_p * L)(*[w.ctypes.data for w in ws])
         bp = (ctypes.c_void_p * L)(*[b.ctypes.data for b in bs])
         h = ctypes.c_void_p()
-        st = _lib.ks_model_create_mlp(self._h, L, _hptr(widths), ctypes.cast(wp, ctypes.c_void_p),
-                                      ctypes.cast(bp, ctypes.c_void_p), _hptr(mu), _hptr(sigma),
-                                      ctypes.byref(h))
-        self._check(st, "ks_model_create_mlp")
+        st = getattr(_lib, name)(self._h, L, _hptr(widths), ctypes.cast(wp, ctypes.c_void_p),
+                                 ctypes.cast(bp, ctypes.c_void_p), _hptr(mu), _hptr(sigma), ctypes.byref(h))
+        self._check(st, name)
         return Model(self, h, "mlp")
 
     def model_create_static(self) -> Model:

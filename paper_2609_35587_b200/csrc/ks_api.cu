@@ -381,6 +381,8 @@ ks_status ks_model_describe(const ks_model* model, char* buf, int len) {
     std::snprintf(buf, len, "select_mlp_tc_kernel");
   } else if (model->kind == 1 && model->mlp.h_ridge) {
     std::snprintf(buf, len, "select_ridge_kernel");
+  } else if (model->kind == 1 && ks::is_e4m3_mlp(model->mlp)) {
+    std::snprintf(buf, len, "matmul_pair_kernel layers=%d", model->mlp.n_layers);
   } else if (model->kind == 1) {
     std::snprintf(buf, len, "mlp_wide_kernel layers=%d", model->mlp.n_layers);
   } else {
@@ -481,13 +483,16 @@ ks_status ks_model_create_gbdt(ks_ctx* ctx, int n_trees, const int64_t* h_tree_o
   }
 }
 
-ks_status ks_model_create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths,
-                              const uint16_t* const* h_w_bf16, const float* const* h_bias,
-                              const float* h_mu, const float* h_sigma, ks_model** out_model) {
+}  // extern "C"
+
+namespace {
+// a feed-forward ranker with its layers in bf16, or (`e4m3`) in eight bits
+ks_status create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths, const uint16_t* const* h_w_bf16, const float* const* h_bias,
+                     const float* h_mu, const float* h_sigma, bool e4m3, const char* what, ks_model** out_model) {
   if (!out_model) return KS_ERR_INVALID_ARG;
   *out_model = nullptr;
   if (!ctx || !h_widths || !h_w_bf16 || !h_bias || !h_mu || !h_sigma) return KS_ERR_INVALID_ARG;
-  if (n_layers < 1 || n_layers > KS_MLP_MAX_LAYERS) return KS_ERR_INVALID_ARG;
+  if (n_layers < (e4m3 ? 2 : 1) || n_layers > KS_MLP_MAX_LAYERS) return KS_ERR_INVALID_ARG;
   const int in0 = h_widths[0];
   if ((in0 != KS_F_PAD && in0 != KS_F_ONEHOT) || h_widths[n_layers] != 1) return KS_ERR_INVALID_ARG;
   for (int l = 1; l < n_layers; ++l) {
@@ -509,17 +514,33 @@ ks_status ks_model_create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths,
     m->kind = 1;
     m->mlp.n_layers = n_layers;
     for (int l = 0; l <= n_layers; ++l) m->mlp.widths[l] = h_widths[l];
-    cudaError_t e = ks::build_fast_mlp(m->mlp, h_w_bf16, h_bias, h_mu, h_sigma);
+    cudaError_t e = e4m3 ? ks::build_e4m3_mlp(m->mlp, h_w_bf16, h_bias, h_mu, h_sigma, &ctx->launches)
+                         : ks::build_fast_mlp(m->mlp, h_w_bf16, h_bias, h_mu, h_sigma);
     // the resident-weights kernel scores given rows in the ordinal input form only
-    if (e == cudaSuccess && !ks::score_mlp_tc_ok(m->mlp)) e = ks::build_wide_mlp(m->mlp, h_w_bf16, h_bias, h_mu, h_sigma);
-    if (e == cudaSuccess) e = ks::build_ridge(m->mlp, h_w_bf16[0], h_bias[0], h_mu, h_sigma);
-    if (e != cudaSuccess) return cuda_fail(ctx, e, "ks_model_create_mlp");
+    if (e == cudaSuccess && !e4m3 && !ks::score_mlp_tc_ok(m->mlp)) e = ks::build_wide_mlp(m->mlp, h_w_bf16, h_bias, h_mu, h_sigma);
+    if (e == cudaSuccess && !e4m3) e = ks::build_ridge(m->mlp, h_w_bf16[0], h_bias[0], h_mu, h_sigma);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, what);
     *out_model = m;
     own.m = nullptr;
     return KS_OK;
   } catch (const std::exception&) {  // (the vectors of the repacking)
     return KS_ERR_OOM;
   }
+}
+}  // namespace
+
+extern "C" {
+
+ks_status ks_model_create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths,
+                              const uint16_t* const* h_w_bf16, const float* const* h_bias,
+                              const float* h_mu, const float* h_sigma, ks_model** out_model) {
+  return create_mlp(ctx, n_layers, h_widths, h_w_bf16, h_bias, h_mu, h_sigma, false, "ks_model_create_mlp", out_model);
+}
+
+ks_status ks_model_create_mlp_e4m3(ks_ctx* ctx, int n_layers, const int* h_widths,
+                                   const uint16_t* const* h_w_bf16, const float* const* h_bias,
+                                   const float* h_mu, const float* h_sigma, ks_model** out_model) {
+  return create_mlp(ctx, n_layers, h_widths, h_w_bf16, h_bias, h_mu, h_sigma, true, "ks_model_create_mlp_e4m3", out_model);
 }
 
 ks_status ks_model_create_static(ks_ctx* ctx, ks_model** out_model) {

@@ -336,6 +336,9 @@ cudaError_t launch_select_mlp_tc(const ks_gpu_desc& desc, const MlpModel& m, con
 // Tensor-core path for rankers of any width (ks_mlp_wide.cu).
 cudaError_t build_wide_mlp(MlpModel& m, const uint16_t* const* h_w, const float* const* h_b, const float* h_mu,
                            const float* h_sigma);
+cudaError_t build_e4m3_mlp(MlpModel& m, const uint16_t* const* h_w, const float* const* h_b, const float* h_mu,
+                           const float* h_sigma, int64_t* launches);  // held in eight bits
+bool is_e4m3_mlp(const MlpModel& m);
 void free_wide_mlp(MlpModel& m);
 int wide_rank_blocks(int64_t per_problem);
 size_t wide_scratch_bytes(const MlpModel& m, int P, int64_t pairs, bool lean);

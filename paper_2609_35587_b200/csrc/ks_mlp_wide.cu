@@ -33,6 +33,7 @@
 #include <new>
 #include <vector>
 
+#include "ks_e4m3.cuh"
 #include "ks_features.cuh"
 #include "ks_internal.h"
 #include "ks_tcgen.cuh"
@@ -56,6 +57,11 @@ struct WideMlp {
   uint8_t* d_image = nullptr;  // weights, then biases (fp32, 1,024 a layer) and the last layer's weights (fp32)
   float b_last = 0.0f;
   WideInput input;
+  // A ranker held in eight bits: its layers are products of ks_matmul8.cu on rows that stay quantised in between, in pieces
+  // of one block of device memory (d_image); max_width is the widest hidden layer.
+  bool e4m3 = false;
+  int max_width = 0;
+  size_t w_at[KS_MLP_MAX_LAYERS] = {0}, ws_at[KS_MLP_MAX_LAYERS] = {0}, b_at[KS_MLP_MAX_LAYERS] = {0}, last_at = 0;
 };
 
 namespace {
@@ -75,7 +81,10 @@ constexpr int64_t kBatchRows = int64_t{55} * kPairs * kRowsPair;  // rows per la
 constexpr int64_t kScorePairs = 64 * kBatchRows;  // scores held at a time (267 MB)
 // ... where the memory for that cannot be had (at most 19 MB in all)
 constexpr int64_t kLeanRows = 8 * kRowsPair, kLeanScorePairs = 512 * kLeanRows;
-constexpr int64_t batch_rows(bool lean) { return lean ? kLeanRows : kBatchRows; }
+// Rows of eight-bit layers at a time: their activations stay in L2, and a layer of 1,024, 512 or 256 units is whole rounds of
+// all pairs of the product's kernel (of 128 columns a half one).
+constexpr int64_t kBatchRowsE4m3 = int64_t{2} * kPairs * kRowsPair;
+int64_t batch_rows(const WideMlp& w, bool lean) { return lean ? kLeanRows : w.e4m3 ? kBatchRowsE4m3 : kBatchRows; }
 constexpr int64_t score_pairs(bool lean) { return lean ? kLeanScorePairs : kScorePairs; }
 constexpr int kTileN = 256;
 
@@ -150,11 +159,63 @@ __device__ __forceinline__ bool epilogue_and(bool v) {
 // the input rows: features (or given rows), standardised, rounded to bf16, in operand form
 // ------------------------------------------------------------------------------------------
 
-// One thread builds one row and writes its 128 (one-hot form: 256) bytes. Rows past the last one up
-// to the end of their 256-row tile are zero.
+// Standardised value of the input position `pos`.
 template <bool kOneHot>
+__device__ __forceinline__ float input_value(const WideInput& in, const float (&x)[KS_F_PAD], bool live, int pos) {
+  float f = 0.0f;
+  bool used;
+  if (!kOneHot) {
+    used = pos < KS_F;
+    if (used) f = x[pos < KS_F ? pos : 0];
+  } else {
+    // the columns other than 5, 9, 17, 18 in order, then the level indicators of those four
+    used = pos < 73;
+    if (pos < 59) {
+      f = x[pos + (pos >= 5) + (pos >= 8) + 2 * (pos >= 15)];
+    } else if (used) {
+      const int p = pos - 59;
+      const int col = p < 4 ? 5 : (p < 7 ? 9 : (p < 11 ? 17 : 18));
+      const int level = p < 4 ? p : (p < 7 ? p - 4 : (p < 11 ? p - 7 : p - 11));
+      f = __float2int_rz(x[col]) == level ? 1.0f : 0.0f;
+    }
+  }
+  if (used) {
+    if (!isfinite(f)) f = 0.0f;
+    f = __fdiv_rn(__fsub_rn(f, in.mu[pos]), in.sigma[pos]);
+  }
+  return used && live ? f : 0.0f;
+}
+
+// One thread builds one row and writes its 128 (one-hot form: 256) bytes. Rows past the last one up
+// to the end of their 256-row tile are zero. For eight-bit layers the row is one block of e4m3 with a scale, 64 (80) bytes, and
+// the scales follow the `n_padded` rows.
+template <bool kOneHot, bool kE4m3>
 __device__ __forceinline__ void store_input_row(const WideInput& in, const float (&x)[KS_F_PAD], bool live, int64_t row,
-                                                uint8_t* image) {
+                                                int64_t n_padded, uint8_t* image) {
+  if constexpr (kE4m3) {
+    constexpr int kWidth = kOneHot ? KS_F_ONEHOT : KS_F_PAD;
+    float v[kWidth], amax = 0.0f;
+#pragma unroll
+    for (int pos = 0; pos < kWidth; ++pos) {
+      v[pos] = input_value<kOneHot>(in, x, live, pos);
+      amax = fmaxf(amax, finite_abs(v[pos]));
+    }
+    uint32_t stored;
+    const float inv = block_scale<true>(amax, stored);
+    uint4* out = reinterpret_cast<uint4*>(image + row * kWidth);
+#pragma unroll
+    for (int c = 0; c < kWidth / 16; ++c) {
+      uint32_t w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float* f = v + 16 * c + 4 * q;
+        w[q] = e4m3_quad(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+      }
+      out[c] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    image[n_padded * kWidth + row] = static_cast<uint8_t>(stored);
+    return;
+  }
   constexpr int kKb = kOneHot ? 2 : 1;
   uint8_t* base = image + (row / kRowsCta) * (kKb * kBlockBytes) + (row % kRowsCta) * 128;
   const int sw = static_cast<int>(row & 7);
@@ -163,34 +224,8 @@ __device__ __forceinline__ void store_input_row(const WideInput& in, const float
     uint32_t w[4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      float v[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int pos = chunk * 8 + 2 * q + h;
-        float f = 0.0f;
-        bool used;
-        if (!kOneHot) {
-          used = pos < KS_F;
-          if (used) f = x[pos < KS_F ? pos : 0];
-        } else {
-          // the columns other than 5, 9, 17, 18 in order, then the level indicators of those four
-          used = pos < 73;
-          if (pos < 59) {
-            f = x[pos + (pos >= 5) + (pos >= 8) + 2 * (pos >= 15)];
-          } else if (used) {
-            const int p = pos - 59;
-            const int col = p < 4 ? 5 : (p < 7 ? 9 : (p < 11 ? 17 : 18));
-            const int level = p < 4 ? p : (p < 7 ? p - 4 : (p < 11 ? p - 7 : p - 11));
-            f = __float2int_rz(x[col]) == level ? 1.0f : 0.0f;
-          }
-        }
-        if (used) {
-          if (!isfinite(f)) f = 0.0f;
-          f = __fdiv_rn(__fsub_rn(f, in.mu[pos]), in.sigma[pos]);
-        }
-        v[h] = (used && live) ? f : 0.0f;
-      }
-      const __nv_bfloat162 t = __floats2bfloat162_rn(v[0], v[1]);
+      const int pos = chunk * 8 + 2 * q;
+      const __nv_bfloat162 t = __floats2bfloat162_rn(input_value<kOneHot>(in, x, live, pos), input_value<kOneHot>(in, x, live, pos + 1));
       w[q] = *reinterpret_cast<const uint32_t*>(&t);
     }
     *reinterpret_cast<uint4*>(base + (chunk / 8) * kBlockBytes + (((chunk & 7) ^ sw) * 16)) =
@@ -206,7 +241,7 @@ wide_terms_kernel(ks_gpu_desc desc, const ks_problem* __restrict__ p, ks_problem
 }
 
 // rows first .. first + n - 1 of the call's pairs
-template <bool kOneHot>
+template <bool kOneHot, bool kE4m3>
 __global__ void __launch_bounds__(128)
 wide_pair_rows_kernel(ks_gpu_desc desc, const ProblemTerms* __restrict__ terms, int P, const ks_candidate* __restrict__ c,
                       int C, const int64_t* __restrict__ seg_off, const int32_t* __restrict__ seg_idx, int64_t first,
@@ -237,10 +272,10 @@ wide_pair_rows_kernel(ks_gpu_desc desc, const ProblemTerms* __restrict__ terms, 
     const ProblemTerms t = terms[prob];
     featurize_pair(t, load_candidate(c + idx), desc, [&](int col, float v) { x[col] = v; });
   }
-  store_input_row<kOneHot>(in, x, live, r, image);
+  store_input_row<kOneHot, kE4m3>(in, x, live, r, n_padded, image);
 }
 
-template <bool kOneHot>
+template <bool kOneHot, bool kE4m3>
 __global__ void __launch_bounds__(128)
 wide_given_rows_kernel(const float* __restrict__ feat, int64_t n, int64_t n_padded,
                        const __grid_constant__ WideInput in, uint8_t* __restrict__ image, int* leave) {
@@ -254,7 +289,7 @@ wide_given_rows_kernel(const float* __restrict__ feat, int64_t n, int64_t n_padd
     const float4 v = __ldg(src + q);
     x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w;
   }
-  store_input_row<kOneHot>(in, x, r < n, r, image);
+  store_input_row<kOneHot, kE4m3>(in, x, r < n, r, n_padded, image);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -527,6 +562,24 @@ mlp_wide_kernel(const __grid_constant__ WideArgs a, const __grid_constant__ CUte
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
+// The last layer of a ranker held in eight bits: a warp per row of the last hidden layer, rounded to bf16.
+__global__ void __launch_bounds__(256) last_layer_kernel(const uint16_t* __restrict__ h, int width, const float* __restrict__ w,
+                                                         float b, int64_t rows, float* __restrict__ scores) {
+  const int64_t row = (static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x) / 32;
+  const int lane = threadIdx.x % 32;
+  if (row >= rows) return;
+  float sum = 0.0f;
+  for (int c = 2 * lane; c < width; c += 64) {  // (widths are multiples of 64)
+    const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(h + row * width + c));
+    const float2 f = __ldg(reinterpret_cast<const float2*>(w + c));
+    sum = fmaf(__uint_as_float(v << 16), f.x, sum);
+    sum = fmaf(__uint_as_float(v & 0xFFFF0000u), f.y, sum);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+  if (lane == 0) scores[row] = (sum + b) + 0.0f;
+}
+
 // ------------------------------------------------------------------------------------------
 // ranking of stored scores
 // ------------------------------------------------------------------------------------------
@@ -589,6 +642,7 @@ cudaError_t make_map(CUtensorMap* map, void* base, int64_t rows, int box_rows) {
 }
 
 size_t image_bytes(const WideMlp& w, int64_t rows) {
+  if (w.e4m3) return static_cast<size_t>((rows + kRowsPair - 1) / kRowsPair * kRowsPair) * ((w.input.onehot ? KS_F_ONEHOT : KS_F_PAD) + 1);
   return static_cast<size_t>((rows + kRowsPair - 1) / kRowsPair) * 2 * kBlockBytes * w.kblocks[0];
 }
 int pairs_used(int64_t rows) {
@@ -600,9 +654,52 @@ int64_t act_rows(const WideMlp& w, int64_t rows) {
   return static_cast<int64_t>(2 * pairs_used(rows)) * 2 * w.max_kb * kRowsCta;
 }
 
+size_t act_bytes(const WideMlp& w, int64_t rows) {
+  // eight bits: two buffers of rows and their scales, and the last hidden layer's rows in bf16
+  if (w.e4m3)
+    return 2 * (up(static_cast<size_t>(rows) * w.max_width) + up(static_cast<size_t>(rows) * scale_blocks(w.max_width))) +
+           up(2 * static_cast<size_t>(rows) * w.width[w.n_hidden - 1]);
+  return static_cast<size_t>(act_rows(w, rows)) * 128;
+}
+
+// the layers of a ranker held in eight bits, over `rows` rows that are quantised at `image`
+cudaError_t launch_layers_e4m3(const WideMlp& w, uint8_t* image, int64_t n_padded, uint8_t* act, int64_t rows, float* scores,
+                               int* status, const FastWait* wait, cudaStream_t stream, int64_t* launches) {
+  const size_t q_bytes = up(static_cast<size_t>(rows) * w.max_width), each = q_bytes + up(static_cast<size_t>(rows) * scale_blocks(w.max_width));
+  int64_t k = w.input.onehot ? KS_F_ONEHOT : KS_F_PAD;
+  MatmulE4m3 p{};
+  p.a = image;
+  p.a_scale = image + n_padded * k;
+  p.scale_type = KS_SCALE_E8M0;
+  p.m = rows;
+  p.relu = 1;
+  for (int l = 0; l < w.n_hidden; ++l) {
+    const bool last = l + 1 == w.n_hidden;
+    uint8_t* out = act + static_cast<size_t>(l & 1) * each;
+    p.lda = p.k = p.ldb = k;
+    p.n = p.ldd = w.width[l];
+    p.b = w.d_image + w.w_at[l];
+    p.b_scale = w.d_image + w.ws_at[l];
+    p.bias = reinterpret_cast<const float*>(w.d_image + w.b_at[l]);
+    p.d = last ? act + 2 * each : out;
+    p.d_type = last ? KS_BF16 : KS_E4M3;
+    p.d_scale = last ? nullptr : out + q_bytes;
+    const cudaError_t e = launch_matmul_e4m3(p, status, stream, launches, wait);
+    if (e != cudaSuccess) return e;
+    p.a = out;
+    p.a_scale = out + q_bytes;
+    k = w.width[l];
+  }
+  last_layer_kernel<<<static_cast<unsigned>((rows + 7) / 8), 256, 0, stream>>>(
+      static_cast<const uint16_t*>(p.d), w.width[w.n_hidden - 1], reinterpret_cast<const float*>(w.d_image + w.last_at), w.b_last, rows, scores);
+  ++*launches;
+  return cudaGetLastError();
+}
+
 // the layers over `rows` rows whose operand image is at `image`
-cudaError_t launch_layers(const WideMlp& w, uint8_t* image, uint8_t* act, int64_t rows, float* scores, int* status,
-                          const FastWait* wait, cudaStream_t stream) {
+cudaError_t launch_layers(const WideMlp& w, uint8_t* image, int64_t n_padded, uint8_t* act, int64_t rows, float* scores, int* status,
+                          const FastWait* wait, cudaStream_t stream, int64_t* launches) {
+  if (w.e4m3) return launch_layers_e4m3(w, image, n_padded, act, rows, scores, status, wait, stream, launches);
   WideArgs a{};
   a.n_hidden = w.n_hidden;
   for (int l = 0; l < w.n_hidden; ++l) {
@@ -629,6 +726,7 @@ cudaError_t launch_layers(const WideMlp& w, uint8_t* image, uint8_t* act, int64_
   if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void*>(&mlp_wide_kernel), kSmemWide);
   if (e != cudaSuccess) return e;
   mlp_wide_kernel<<<2 * pairs_used(rows), kThreads, kSmemWide, stream>>>(a, mx, ma, mw[0], mw[1], mw[2], mw[3]);
+  ++*launches;
   return cudaGetLastError();
 }
 
@@ -688,12 +786,68 @@ cudaError_t build_wide_mlp(MlpModel& m, const uint16_t* const* h_w, const float*
   return e;
 }
 
+// The same of a ranker held in eight bits: its hidden layers' weights are quantised on the device, in blocks of 128 x 128 with
+// a power of two as scale.
+cudaError_t build_e4m3_mlp(MlpModel& m, const uint16_t* const* h_w, const float* const* h_b, const float* h_mu,
+                           const float* h_sigma, int64_t* launches) {
+  WideMlp* w = new (std::nothrow) WideMlp();
+  if (!w) return cudaErrorMemoryAllocation;
+  m.wide = w;
+  w->e4m3 = true;
+  w->n_hidden = m.n_layers - 1;
+  w->kblocks[0] = (m.widths[0] + 63) / 64;
+  w->b_last = h_b[m.n_layers - 1][0];
+  w->input.onehot = m.widths[0] == KS_F_ONEHOT;
+  for (int j = 0; j < KS_F_ONEHOT; ++j) {
+    w->input.mu[j] = j < m.widths[0] ? h_mu[j] : 0.0f;
+    w->input.sigma[j] = j < m.widths[0] ? h_sigma[j] : 1.0f;
+  }
+  size_t bytes = 0, most = 0;
+  for (int l = 0; l < w->n_hidden; ++l) {
+    const size_t in = m.widths[l], out = m.widths[l + 1];
+    w->width[l] = m.widths[l + 1];
+    w->max_width = std::max(w->max_width, w->width[l]);
+    w->w_at[l] = bytes;
+    bytes += up(in * out);
+    w->ws_at[l] = bytes;
+    bytes += up(static_cast<size_t>(scale_blocks(in) * scale_blocks(out)));
+    w->b_at[l] = bytes;
+    bytes += up(out * sizeof(float));
+    most = std::max(most, 2 * in * out);
+  }
+  w->last_at = bytes;
+  const int width = m.widths[m.n_layers - 1];
+  std::vector<float> last(width);
+  for (int n = 0; n < width; ++n) {
+    const uint32_t u = static_cast<uint32_t>(h_w[m.n_layers - 1][n]) << 16;
+    std::memcpy(&last[n], &u, 4);
+  }
+  bytes += up(width * sizeof(float));
+  uint8_t* bf16 = nullptr;  // a layer's weights as given
+  cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&w->d_image), bytes);
+  if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&bf16), most);
+  for (int l = 0; l < w->n_hidden && e == cudaSuccess; ++l) {
+    const int64_t in = m.widths[l], out = m.widths[l + 1];
+    e = cudaMemcpy(bf16, h_w[l], 2 * in * out, cudaMemcpyHostToDevice);
+    if (e == cudaSuccess)
+      e = launch_quantize_e4m3(bf16, KS_BF16, out, in, in, kScaleBlock, KS_SCALE_E8M0, w->d_image + w->w_at[l], in,
+                               w->d_image + w->ws_at[l], nullptr, launches);
+    if (e == cudaSuccess) e = cudaMemcpy(w->d_image + w->b_at[l], h_b[l], out * sizeof(float), cudaMemcpyHostToDevice);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
+  }
+  if (e == cudaSuccess) e = cudaMemcpy(w->d_image + w->last_at, last.data(), width * sizeof(float), cudaMemcpyHostToDevice);
+  cudaFree(bf16);
+  return e;
+}
+
 void free_wide_mlp(MlpModel& m) {
   if (!m.wide) return;
   cudaFree(m.wide->d_image);
   delete m.wide;
   m.wide = nullptr;
 }
+
+bool is_e4m3_mlp(const MlpModel& m) { return m.wide && m.wide->e4m3; }
 
 int wide_rank_blocks(int64_t per_problem) {
   const int64_t n = (per_problem + kRankRows - 1) / kRankRows;
@@ -702,9 +856,9 @@ int wide_rank_blocks(int64_t per_problem) {
 
 // problem terms | scores of a round's pairs | operand image of a batch | activations
 size_t wide_scratch_bytes(const MlpModel& m, int P, int64_t pairs, bool lean) {
-  const int64_t batch = std::min(pairs, batch_rows(lean));
+  const int64_t batch = std::min(pairs, batch_rows(*m.wide, lean));
   return up(sizeof(ProblemTerms) * static_cast<size_t>(P > 0 ? P : 1)) + up(sizeof(float) * static_cast<size_t>(std::min(pairs, score_pairs(lean)))) +
-         up(image_bytes(*m.wide, batch)) + static_cast<size_t>(act_rows(*m.wide, batch)) * 128 + 1024;
+         up(image_bytes(*m.wide, batch)) + act_bytes(*m.wide, batch) + 1024;
 }
 
 cudaError_t launch_select_wide(const ks_gpu_desc& desc, const MlpModel& m, const ks_problem* d_p,
@@ -713,7 +867,7 @@ cudaError_t launch_select_wide(const ks_gpu_desc& desc, const MlpModel& m, const
                                unsigned long long* partial, void* scratch, int* status, cudaStream_t stream,
                                int64_t* launches, cudaEvent_t ev_begin, const FastWait* wait) {
   const WideMlp& w = *m.wide;
-  const int64_t batch = batch_rows(wait->lean), round = score_pairs(wait->lean);
+  const int64_t batch = batch_rows(w, wait->lean), round = score_pairs(wait->lean);
   char* q = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(scratch) + 1023) / 1024 * 1024);
   ProblemTerms* terms = reinterpret_cast<ProblemTerms*>(q);
   q += up(sizeof(ProblemTerms) * static_cast<size_t>(P));
@@ -733,16 +887,14 @@ cudaError_t launch_select_wide(const ks_gpu_desc& desc, const MlpModel& m, const
     for (; first < round_end; first += batch) {
       const int64_t n = std::min(round_end - first, batch), padded = (n + kRowsPair - 1) / kRowsPair * kRowsPair;
       const unsigned grid = static_cast<unsigned>((padded + 127) / 128);
-      if (w.input.onehot)
-        wide_pair_rows_kernel<true><<<grid, 128, 0, stream>>>(desc, terms, P, d_c, C, seg_off, seg_idx, first, n, padded,
-                                                              w.input, image, wait->words + kWordWide);
-      else
-        wide_pair_rows_kernel<false><<<grid, 128, 0, stream>>>(desc, terms, P, d_c, C, seg_off, seg_idx, first, n,
-                                                               padded, w.input, image, wait->words + kWordWide);
+      const auto rows_kernel = w.e4m3 ? (w.input.onehot ? wide_pair_rows_kernel<true, true> : wide_pair_rows_kernel<false, true>)
+                                      : (w.input.onehot ? wide_pair_rows_kernel<true, false> : wide_pair_rows_kernel<false, false>);
+      rows_kernel<<<grid, 128, 0, stream>>>(desc, terms, P, d_c, C, seg_off, seg_idx, first, n, padded, w.input, image,
+                                            wait->words + kWordWide);
+      ++*launches;
       cudaError_t e = cudaGetLastError();
-      if (e == cudaSuccess) e = launch_layers(w, image, act, n, scores + (first - round0), status, wait, stream);
+      if (e == cudaSuccess) e = launch_layers(w, image, padded, act, n, scores + (first - round0), status, wait, stream, launches);
       if (e != cudaSuccess) return e;
-      *launches += 2;
     }
     rank_scores_kernel<<<static_cast<unsigned>(static_cast<int64_t>(P) * nblk), kBlock, 0, stream>>>(
         scores, round0, round_end - round0, round0 == 0, C, nblk, seg_off, seg_idx, k, partial);
@@ -752,26 +904,27 @@ cudaError_t launch_select_wide(const ks_gpu_desc& desc, const MlpModel& m, const
 }
 
 size_t score_wide_scratch_bytes(const MlpModel& m, int64_t rows, bool lean) {
-  const int64_t batch = std::min(rows, batch_rows(lean));
-  return up(image_bytes(*m.wide, batch)) + static_cast<size_t>(act_rows(*m.wide, batch)) * 128 + 1024;
+  const int64_t batch = std::min(rows, batch_rows(*m.wide, lean));
+  return up(image_bytes(*m.wide, batch)) + act_bytes(*m.wide, batch) + 1024;
 }
 
 cudaError_t launch_score_wide(const MlpModel& m, const float* d_feat, int64_t rows, float* d_scores, void* scratch,
                               int* status, cudaStream_t stream, int64_t* launches, const FastWait* wait) {
   const WideMlp& w = *m.wide;
-  const int64_t batch = batch_rows(wait->lean);
+  const int64_t batch = batch_rows(w, wait->lean);
   uint8_t* image = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(scratch) + 1023) / 1024 * 1024);
   uint8_t* act = image + up(image_bytes(w, std::min(rows, batch)));
   for (int64_t first = 0; first < rows; first += batch) {
     const int64_t n = std::min(rows - first, batch), padded = (n + kRowsPair - 1) / kRowsPair * kRowsPair;
     const unsigned grid = static_cast<unsigned>((padded + 127) / 128);
     const float* x = d_feat + first * KS_F_PAD;
-    if (w.input.onehot) wide_given_rows_kernel<true><<<grid, 128, 0, stream>>>(x, n, padded, w.input, image, wait->words + kWordWide);
-    else wide_given_rows_kernel<false><<<grid, 128, 0, stream>>>(x, n, padded, w.input, image, wait->words + kWordWide);
+    const auto rows_kernel = w.e4m3 ? (w.input.onehot ? wide_given_rows_kernel<true, true> : wide_given_rows_kernel<false, true>)
+                                    : (w.input.onehot ? wide_given_rows_kernel<true, false> : wide_given_rows_kernel<false, false>);
+    rows_kernel<<<grid, 128, 0, stream>>>(x, n, padded, w.input, image, wait->words + kWordWide);
+    ++*launches;
     cudaError_t e = cudaGetLastError();
-    if (e == cudaSuccess) e = launch_layers(w, image, act, n, d_scores + first, status, wait, stream);
+    if (e == cudaSuccess) e = launch_layers(w, image, padded, act, n, d_scores + first, status, wait, stream, launches);
     if (e != cudaSuccess) return e;
-    *launches += 2;
   }
   return cudaSuccess;
 }

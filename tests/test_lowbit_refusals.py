@@ -92,3 +92,20 @@ def test_sampling_records_are_the_c_struct():
     r["temperature"], r["top_k"], r["top_p"], r["min_p"] = 0.5, 7, 0.25, 0.125
     s = ks._Sampling.from_buffer_copy(r.tobytes())
     assert (s.temperature, s.top_k, s.top_p, s.min_p) == (0.5, 7, 0.25, 0.125)
+
+
+def test_model_in_eight_bits():
+    widths = np.array([64, 64, 1], np.int32)
+    one = np.ones(64 * 64, np.float32)
+    w = (ctypes.c_void_p * 2)(P, P)
+    out = ctypes.c_void_p()
+
+    def create(n_layers, widths, sigma=one):
+        return call(ks._lib.ks_model_create_mlp_e4m3, n_layers, widths.ctypes.data, ctypes.cast(w, ctypes.c_void_p),
+                    ctypes.cast(w, ctypes.c_void_p), one.ctypes.data, sigma.ctypes.data, ctypes.byref(out))
+    assert create(1, np.array([64, 1], np.int32)) == ks.KS_ERR_INVALID_ARG  # a linear scorer has no layer to quantise
+    assert create(2, np.array([64, 100, 1], np.int32)) == ks.KS_ERR_INVALID_ARG
+    assert create(2, np.array([72, 64, 1], np.int32)) == ks.KS_ERR_INVALID_ARG
+    assert create(7, widths) == ks.KS_ERR_INVALID_ARG
+    assert create(2, widths, np.zeros(64, np.float32)) == ks.KS_ERR_INVALID_ARG
+    assert out.value is None
