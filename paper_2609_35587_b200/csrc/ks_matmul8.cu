@@ -147,25 +147,24 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kChunk = 8;  // blocks of K whose scales are brought together
 constexpr int kCols = 64;  // of an epilogue warp
 constexpr int kStorePitch = 9;
+struct Tile {
+  int m, n;
+};
 struct PairShared {  // behind the stages
   float a_scale[2][kChunk][kHalf];
   float b_scale[2][2][kChunk];
   float bias[2][kTile];
+  Tile tile[2];
   float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 32-byte boundaries
   float amax[2][16][32];  // of a warp's rows, for the one that has the block's other half
 };
 constexpr int kSmem = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(PairShared));
 constexpr int kGroup = 8;  // row tiles that share a stretch of column tiles, for L2
 
-struct Tile {
-  int m, n;
-};
-__device__ __forceinline__ Tile tile_at(int64_t t, int tiles_m, int tiles_n) {
-  const int64_t per = static_cast<int64_t>(kGroup) * tiles_n;
-  const int first = static_cast<int>(t / per) * kGroup;
-  const int rows = tiles_m - first < kGroup ? tiles_m - first : kGroup;
-  const int in = static_cast<int>(t % per);
-  return Tile{(first + in % rows) * kTile, (in / rows) * kTile};
+__device__ __forceinline__ Tile tile_at(uint32_t t, uint32_t tiles_m, uint32_t tiles_n) {
+  const uint32_t per = kGroup * tiles_n, group = t / per, in = t - group * per, first = group * kGroup;
+  const uint32_t rows = tiles_m - first < kGroup ? tiles_m - first : kGroup, col = in / rows;
+  return Tile{static_cast<int>((first + in - col * rows) * kTile), static_cast<int>(col * kTile)};
 }
 
 // Bias and ReLU on a thread's 64 neighbouring elements of a row.
@@ -252,7 +251,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = blockIdx.x & 1;  // CTA of the pair; 0 issues the MMAs
-  const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  const uint32_t pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
   unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
   PairShared& sh = *reinterpret_cast<PairShared*>(smem + kStages * kStageBytes);
   const uint32_t sbase = smem_addr(smem), bar0 = smem_addr(&s_bar[0]);
@@ -289,7 +288,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   fence_after();
   const uint32_t tmem = s_tmem;
   const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
-  const int64_t tiles = static_cast<int64_t>(tiles_m) * tiles_n;
+  const uint32_t tiles = static_cast<uint32_t>(tiles_m) * tiles_n;  // (checked by the host)
   const int chunks = p.kblocks > 0 ? (p.kblocks + kChunk - 1) / kChunk : 1;
   volatile int* v_fail = &s_fail;
 
@@ -314,7 +313,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
       const bool lead = elect_one();
       uint32_t s = 0, parity = 1;
       bool ok = true;
-      for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+      for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
         const Tile at = tile_at(t, tiles_m, tiles_n);
         const int row_a = at.m + static_cast<int>(rank) * kHalf, row_b = at.n + static_cast<int>(rank) * kHalf;
         for (int kb = 0; kb < p.kblocks; ++kb) {
@@ -341,7 +340,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
         bool ok = true;
         constexpr uint32_t idesc = instr_desc(kTile, kTile);
         const uint64_t desc0 = operand_desc(sbase);
-        for (int64_t t = pair; t < tiles && ok; t += n_pairs) {
+        for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
           for (int kb = 0; kb < p.kblocks; ++kb) {
             if (!(ok = wait_ok(bar_read(acc), parity_acc) && wait_ok(bar_full(s), parity))) break;
             fence_after();
@@ -370,12 +369,13 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
       uint32_t it = 0;
       bool ok = true;
       uint32_t tile_par = 0;
-      for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
+      for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
         const Tile at = tile_at(t, tiles_m, tiles_n);
         for (int c = 0; c < chunks; ++c, ++it) {
           const uint32_t buf = it & 1u;
           if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_used(buf), ((it >> 1) & 1u) ^ 1u)))) break;
           const int kb0 = c * kChunk, n_kb = p.kblocks - kb0 < kChunk ? p.kblocks - kb0 : kChunk;
+          if (c == 0 && warp == 2 && lane == 0) sh.tile[tile_par] = at;
           if (c == 0 && p.bias)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -415,10 +415,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     };
     uint32_t it = 0, tile_par = 0;
     bool ok = true;
-    for (int64_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
-      const Tile at = tile_at(t, tiles_m, tiles_n);
-      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + part * kCols;
-      const bool inside = n0 < p.n;  // (of the warp's columns any)
+    for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u) {
       float sum[kCols];
 #pragma unroll
       for (int q = 0; q < kCols; ++q) sum[q] = 0.0f;
@@ -453,6 +450,9 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
         }
       }
       if (!ok) break;
+      const Tile at = sh.tile[tile_par];
+      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + part * kCols;
+      const bool inside = n0 < p.n;  // (of the warp's columns any)
       finish_block(p, sum, sh.bias[tile_par] + part * kCols);
       bool odd = false;
       if (kType == KS_E4M3) {  // the block's other 64 columns are another warp's
@@ -728,6 +728,7 @@ cudaError_t launch_pair(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t s
   if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void*>(&matmul_pair_kernel<kType>), kSmem);
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((q.m + kTile - 1) / kTile) * ((q.n + kTile - 1) / kTile);
+  if (tiles + kSms > UINT32_MAX) return cudaErrorInvalidConfiguration;
   matmul_pair_kernel<kType><<<2 * static_cast<int>(std::min<int64_t>(tiles, kSms / 2)), kThreads, kSmem, stream>>>(p, ma, mb);
   return cudaGetLastError();
 }
