@@ -29,10 +29,6 @@ __device__ __forceinline__ float scale_value(const void* s, int64_t at, int type
 __device__ __forceinline__ void add_scaled(Wide& sum, uint32_t lo, uint32_t hi, Wide s) {
   asm("{\n .reg .b64 t;\n mov.b64 t, {%1, %2};\n fma.rn.f32x2 %0, t, %3, %0;\n}\n" : "+l"(sum) : "r"(lo), "r"(hi), "l"(s));
 }
-__device__ __forceinline__ Wide both(float v) {
-  const uint32_t u = __float_as_uint(v);
-  return (static_cast<Wide>(u) << 32) | u;
-}
 __device__ __forceinline__ float low(Wide v) { return __uint_as_float(static_cast<uint32_t>(v)); }
 __device__ __forceinline__ float high(Wide v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); }
 
@@ -455,13 +451,311 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
       const bool inside = n0 < p.n;  // (of the warp's columns any)
       finish_block(p, sum, sh.bias[tile_par] + part * kCols);
       bool odd = false;
+      float amax = 0.0f;
+      if (kType == KS_E4M3) {  // the block's other 64 columns are another warp's
+        amax = block_max(sum, odd);
+        sh.amax[tile_par][warp - 4][lane] = amax;
+        __syncwarp();
+        const int which = j * 4 + quarter;
+        if (lane == 0) bar_arrive(bar_max(which));
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_max(which), tile_par)))) break;
+        amax = fmaxf(amax, sh.amax[tile_par][(warp - 4) ^ 4][lane]);
+      }
+      // (with the last chunk's scales the bias is read too; behind the stores the arrival would wait for them)
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_used((it - 1) & 1u));
+      if (kType == KS_E4M3) {
+        const float inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock,
+                                       row < p.m && inside && !(part & 1));
+#pragma unroll
+        for (int q = 0; q < kCols; ++q) sum[q] *= inv;
+      }
+      if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
+    }
+  }
+  // after a failure: time for the copies and MMAs in flight to end
+  if (*v_fail)
+    for (int i = 0; i < 64; ++i) __nanosleep(2000);
+  __syncthreads();
+  cluster_sync();
+  if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// ------------------------------------------------------------------------------------------
+// many rows, scales that are powers of two: the tensor core multiplies them in
+// ------------------------------------------------------------------------------------------
+
+// The same tiles, with MMAs that take a power of two for each row of A, row of B and 32 of K (of a block of 128 the same four
+// times) from tensor memory. So one accumulator takes a whole part of K and is read once: of the 26,000 instructions that a
+// tile of K = 1,024 takes an SM in matmul_pair_kernel, 17,000 read the accumulators of its blocks. The tensor core adds by
+// truncation, so a part is 4,096 of K at most (128 additions, each off by 2^-24 at most), and the parts are added in registers.
+// The scales' places leave room for one accumulator: the MMAs stand still while it is read into registers, 700 clocks of the
+// 4,100 of K = 1,024, but not while a tile is finished and written.
+constexpr int kPart = 32;         // blocks of K that an accumulator takes
+constexpr int kWords = 4;         // blocks of K whose scales are in a word
+constexpr int kScaleBuffers = 4;
+constexpr int kScaleBytes = 3 * 512;  // of a CTA's 128 rows and of both blocks of 128 columns
+constexpr int kScaleColumn = 256;     // of tensor memory, 32 columns a buffer
+struct ScaledShared {  // behind the stages
+  alignas(128) uint8_t scale[kScaleBuffers][kScaleBytes];
+  alignas(16) float bias[2][kTile];
+  Tile tile[2];
+  float store[16][32 * kStorePitch];
+  float amax[2][16][32];
+};
+constexpr int kSmemScaled = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(ScaledShared));
+
+// D fp32, A and B e4m3, K-major, scales e8m0; of their words byte `k`
+__device__ __forceinline__ uint32_t scaled_desc(int m, int n, uint32_t k) {
+  return instr_desc(m, n) & ~(1u << 4) | (k << 4) | (1u << 23) | (k << 29);
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+      : "memory");
+}
+// 32 rows of 16 bytes to four columns of tensor memory in both CTAs, the same for each quarter of the lanes
+__device__ __forceinline__ void copy_scales(uint32_t column, uint32_t saddr) {
+  const uint64_t desc = static_cast<uint64_t>((saddr >> 4) & 0x3FFFu) | (1ull << 16) | (8ull << 32) | (1ull << 46);  // groups of eight rows 128 bytes apart
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(column), "l"(desc) : "memory");
+}
+
+template <int kType>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
+                     const __grid_constant__ CUtensorMap map_b) {
+  extern __shared__ unsigned char smem_raw[];
+  // full[kStages] (the leader's are used), empty[kStages], scales full[kScaleBuffers] (the leader's) and used[kScaleBuffers],
+  // accumulator full and read out (the leader's), bias there[2] and read[2], halves of a block's maxima [8]
+  constexpr int kBars = 2 * kStages + 2 * kScaleBuffers + 2 + 4 + 8;
+  __shared__ __align__(16) Wide s_bar[kBars];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_fail;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = blockIdx.x & 1;  // CTA of the pair; 0 issues the MMAs
+  const uint32_t pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
+  unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
+  ScaledShared& sh = *reinterpret_cast<ScaledShared*>(smem + kStages * kStageBytes);
+  const uint32_t sbase = smem_addr(smem), bar0 = smem_addr(&s_bar[0]);
+  auto bar_full = [&](int s) { return bar0 + 8u * s; };
+  auto bar_empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+  constexpr int kAt = 2 * kStages;
+  auto bar_scale = [&](uint32_t i) { return bar0 + 8u * (kAt + i); };
+  auto bar_used = [&](uint32_t i) { return bar0 + 8u * (kAt + kScaleBuffers + i); };
+  const uint32_t bar_acc = bar0 + 8u * (kAt + 2 * kScaleBuffers), bar_read = bar_acc + 8u;
+  auto bar_bias = [&](uint32_t i) { return bar_read + 8u * (1 + i); };
+  auto bar_bias_read = [&](uint32_t i) { return bar_read + 8u * (3 + i); };
+  auto bar_max = [&](int i) { return bar_read + 8u * (5 + i); };
+
+  if (tid == 0) {
+    s_fail = 0;
+    for (int s = 0; s < kStages; ++s) {
+      bar_init(bar_full(s), 1);
+      bar_init(bar_empty(s), 1);
+    }
+    for (int i = 0; i < kScaleBuffers; ++i) {
+      bar_init(bar_scale(i), 4);  // two warps of each CTA
+      bar_init(bar_used(i), 1);
+    }
+    bar_init(bar_acc, 1);
+    bar_init(bar_read, 32);  // sixteen epilogue warps of each CTA
+    for (int i = 0; i < 2; ++i) {
+      bar_init(bar_bias(i), 2);
+      bar_init(bar_bias_read(i), 16);
+    }
+    for (int i = 0; i < 8; ++i) bar_init(bar_max(i), 2);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  cluster_sync();  // both CTAs' barriers exist before either is used
+  fence_after();
+  const uint32_t tmem = s_tmem;
+  const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
+  const uint32_t tiles = static_cast<uint32_t>(tiles_m) * tiles_n;
+  volatile int* v_fail = &s_fail;
+  auto wait_ok = [&](uint32_t bar, uint32_t parity) {  // (as in matmul_pair_kernel)
+    if (bar_try_tmem(bar, parity)) return true;
+    for (int i = 0; i < p.wait_limit; ++i) {
+      if (bar_try_tmem(bar, parity)) return true;
+      if ((i & 63) == 63 && *v_fail) return false;
+    }
+    *v_fail = 1;
+    if (p.status) atomicExch(p.status, KS_ERR_TIMEOUT);
+    return false;
+  };
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsFew));
+    if (warp == 0) {
+      const bool lead = elect_one();
+      uint32_t s = 0, parity = 1;
+      bool ok = true;
+      for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
+        const Tile at = tile_at(t, tiles_m, tiles_n);
+        const int row_a = at.m + static_cast<int>(rank) * kHalf, row_b = at.n + static_cast<int>(rank) * kHalf;
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+          if (!(ok = wait_ok(bar_empty(s), parity))) break;
+          const uint32_t full = to_cluster(bar_full(s), 0), dst = sbase + s * kStageBytes;
+          if (lead) {
+            if (rank == 0) bar_expect(bar_full(s), 2u * kStageBytes);
+            if (!p.starve) {  // test hook: without the copies the waits on this barrier run out
+              load_pair(dst, &map_a, kb * kScaleBlock, row_a, full);
+              load_pair(dst + kOperandBytes, &map_b, kb * kScaleBlock, row_b, full);
+            }
+          }
+          if (++s == kStages) {
+            s = 0;
+            parity ^= 1u;
+          }
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      if (rank == 0) {
+        const bool lead = elect_one();
+        uint32_t s = 0, parity = 0, parity_acc = 1, buf = 0, parity_scale = 0;
+        bool ok = true;
+        const uint64_t desc0 = operand_desc(sbase);
+        const uint32_t scale0 = smem_addr(&sh.scale[0][0]);
+        for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
+          for (int kb = 0; kb < p.kblocks; ++kb) {
+            const uint32_t sa = tmem + kScaleColumn + 32u * buf, sb = sa + 16u;
+            if (kb % kWords == 0) {
+              // (a buffer that is filled again has been used: the warps that fill it waited for its MMAs. The peer's threads
+              // wrote half of it)
+              while (ok && !bar_try(bar_scale(buf), parity_scale)) ok = wait_ok(bar_scale(buf), parity_scale);
+              if (!ok) break;
+              if (lead)
+#pragma unroll
+                for (int i = 0; i < 3; ++i) copy_scales(sa + (i == 0 ? 0 : 12 + 4 * i), scale0 + buf * kScaleBytes + i * 512);
+            }
+            if (kb % kPart == 0 && !(ok = wait_ok(bar_read, parity_acc))) break;
+            if (!(ok = wait_ok(bar_full(s), parity))) break;
+            fence_after();
+            const uint64_t da = desc0 + s * (kStageBytes >> 4), db = da + (kOperandBytes >> 4);
+            const uint32_t idesc = scaled_desc(kTile, kTile, kb % kWords);
+            const bool part_ends = kb + 1 == p.kblocks || (kb + 1) % kPart == 0;
+            const bool word_ends = kb + 1 == p.kblocks || (kb + 1) % kWords == 0;
+            if (lead) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
+                mma_scaled(tmem, da + 2u * k, db + 2u * k, idesc, sa, sb, k > 0 || kb % kPart > 0);
+              commit_pair(bar_empty(s));
+              if (word_ends) commit_pair(bar_used(buf));
+              if (part_ends) commit_pair(bar_acc);
+            }
+            if (part_ends) parity_acc ^= 1u;
+            if (word_ends && ++buf == kScaleBuffers) {
+              buf = 0;
+              parity_scale ^= 1u;
+            }
+            if (++s == kStages) {
+              s = 0;
+              parity ^= 1u;
+            }
+          }
+        }
+      }
+      __syncwarp();
+    } else {
+      // scales of this CTA's rows (two rows a thread) and of one of the blocks of columns; a tile's place and bias
+      const int j = warp - 2, r0 = j * 64 + lane;
+      uint32_t buf = 0, parity_used = 1, tile_par = 0, tile_count = 0;
+      bool ok = true;
+      const bool words = p.kblocks % kWords == 0 && reinterpret_cast<uintptr_t>(p.a_scale) % 4 == 0 && reinterpret_cast<uintptr_t>(p.b_scale) % 4 == 0;
+      auto word_at = [&](const void* scales, int64_t at, int n_kb) {
+        const uint8_t* from = static_cast<const uint8_t*>(scales) + at;
+        if (words) return __ldg(reinterpret_cast<const uint32_t*>(from));
+        uint32_t w = 0;
+#pragma unroll
+        for (int k = 0; k < kWords; ++k)
+          if (k < n_kb) w |= static_cast<uint32_t>(__ldg(from + k)) << (8 * k);
+        return w;
+      };
+      for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u, ++tile_count) {
+        const Tile at = tile_at(t, tiles_m, tiles_n);
+        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_bias_read(tile_par), ((tile_count >> 1) & 1u) ^ 1u)))) break;
+        if (j == 0 && lane == 0) sh.tile[tile_par] = at;
+        for (int i = 0; i < 4; ++i) {
+          const int n = j * kHalf + 32 * i + lane;
+          sh.bias[tile_par][n] = p.bias && at.n + n < p.n ? __ldg(p.bias + at.n + n) : 0.0f;
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(bar_bias(tile_par));
+        const int row = at.m + static_cast<int>(rank) * kHalf + r0, nb = at.n / kScaleBlock + j;
+        for (int kb = 0; kb < p.kblocks; kb += kWords) {
+          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_used(buf), parity_used)))) break;
+          const int n_kb = p.kblocks - kb;
+          const uint32_t w0 = row < p.m ? word_at(p.a_scale, static_cast<int64_t>(row) * p.kblocks + kb, n_kb) : 0u;
+          const uint32_t w1 = row + 32 < p.m ? word_at(p.a_scale, static_cast<int64_t>(row + 32) * p.kblocks + kb, n_kb) : 0u;
+          const uint32_t wb = nb * kScaleBlock < p.n ? word_at(p.b_scale, static_cast<int64_t>(nb) * p.kblocks + kb, n_kb) : 0u;
+          uint32_t* out = reinterpret_cast<uint32_t*>(sh.scale[buf]);
+          // row r of 128: 16 bytes a lane r % 32, word r / 32 of them
+          out[lane * 4 + 2 * j] = w0;
+          out[lane * 4 + 2 * j + 1] = w1;
+          *reinterpret_cast<uint4*>(out + 128 + 128 * j + 4 * lane) = make_uint4(wb, wb, wb, wb);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(to_cluster(bar_scale(buf), 0));
+          if (++buf == kScaleBuffers) {
+            buf = 0;
+            parity_used ^= 1u;
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsEpilogue));
+    const int quarter = warp & 3, part = (warp - 4) >> 2, j = part >> 1;  // (as in matmul_pair_kernel)
+    const int trow = quarter * 32 + lane;
+    const uint32_t acc_col = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + part * kCols;
+    const uint32_t read_bar = to_cluster(bar_read, 0), first = lane == 0;
+    auto warp_wait = [&](uint32_t bar, uint32_t parity) {
+      return bar_try_warp(bar, parity) || __all_sync(0xFFFFFFFFu, wait_ok(bar, parity));
+    };
+    uint32_t acc_parity = 0, tile_par = 0, tile_count = 0;
+    bool ok = true;
+    for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u, ++tile_count) {
+      float sum[kCols];
+#pragma unroll
+      for (int q = 0; q < kCols; ++q) sum[q] = 0.0f;
+      for (int kb = 0; kb < p.kblocks; kb += kPart) {
+        if (!(ok = warp_wait(bar_acc, acc_parity))) break;
+        acc_parity ^= 1u;
+        fence_after();
+        uint32_t r[32];
+        tmem_read32(acc_col, r);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) sum[q] += __uint_as_float(r[q]);
+        tmem_read32(acc_col + 32, r);
+        fence_before();
+        bar_arrive_tmem_if(read_bar, first);
+#pragma unroll
+        for (int q = 0; q < 32; ++q) sum[32 + q] += __uint_as_float(r[q]);
+      }
+      if (!ok || !(ok = warp_wait(bar_bias(tile_par), (tile_count >> 1) & 1u))) break;
+      const Tile at = sh.tile[tile_par];
+      const int row = at.m + static_cast<int>(rank) * kHalf + trow, n0 = at.n + part * kCols;
+      const bool inside = n0 < p.n;  // (of the warp's columns any)
+      finish_block(p, sum, sh.bias[tile_par] + part * kCols);
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_bias_read(tile_par));
+      bool odd = false;
       if (kType == KS_E4M3) {  // the block's other 64 columns are another warp's
         float amax = block_max(sum, odd);
         sh.amax[tile_par][warp - 4][lane] = amax;
         __syncwarp();
         const int which = j * 4 + quarter;
         if (lane == 0) bar_arrive(bar_max(which));
-        if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_max(which), tile_par)))) break;
+        if (!(ok = warp_wait(bar_max(which), tile_par))) break;
         amax = fmaxf(amax, sh.amax[tile_par][(warp - 4) ^ 4][lane]);
         const float inv = stored_scale(p, amax, static_cast<int64_t>(row) * scale_blocks(p.n) + n0 / kScaleBlock,
                                        row < p.m && inside && !(part & 1));
@@ -469,8 +763,6 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
         for (int q = 0; q < kCols; ++q) sum[q] *= inv;
       }
       if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
-      __syncwarp();
-      if (lane == 0) bar_arrive(bar_used((it - 1) & 1u));  // (with the last chunk's scales the bias is read too)
     }
   }
   // after a failure: time for the copies and MMAs in flight to end
@@ -713,23 +1005,26 @@ cudaError_t make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t k
              : cudaErrorInvalidValue;
 }
 
-template <int kType>
+template <int kType, bool kScaled>
 cudaError_t launch_pair(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
+  void (*const kernel)(MatmulArgs, CUtensorMap, CUtensorMap) = kScaled ? &matmul_scaled_kernel<kType> : &matmul_pair_kernel<kType>;
+  const void* address = reinterpret_cast<const void*>(kernel);
   // the register split is made for this count
-  static const cudaError_t fits = [] {
+  static const cudaError_t fits = [address] {
     cudaFuncAttributes attr{};
-    const cudaError_t e = cudaFuncGetAttributes(&attr, reinterpret_cast<const void*>(&matmul_pair_kernel<kType>));
+    const cudaError_t e = cudaFuncGetAttributes(&attr, address);
     return e != cudaSuccess ? e : attr.numRegs == kRegs ? cudaSuccess : cudaErrorInvalidKernelImage;
   }();
   if (fits != cudaSuccess) return fits;
+  constexpr int kBytes = kScaled ? kSmemScaled : kSmem;
   CUtensorMap ma, mb;
   cudaError_t e = make_map(&ma, q.a, q.m, q.k, q.lda, kHalf);
   if (e == cudaSuccess) e = make_map(&mb, q.b, q.n, q.k, q.ldb, kHalf);
-  if (e == cudaSuccess) e = ensure_dynamic_smem(reinterpret_cast<const void*>(&matmul_pair_kernel<kType>), kSmem);
+  if (e == cudaSuccess) e = ensure_dynamic_smem(address, kBytes);
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((q.m + kTile - 1) / kTile) * ((q.n + kTile - 1) / kTile);
   if (tiles + kSms > UINT32_MAX) return cudaErrorInvalidConfiguration;
-  matmul_pair_kernel<kType><<<2 * static_cast<int>(std::min<int64_t>(tiles, kSms / 2)), kThreads, kSmem, stream>>>(p, ma, mb);
+  kernel<<<2 * static_cast<int>(std::min<int64_t>(tiles, kSms / 2)), kThreads, kBytes, stream>>>(p, ma, mb);
   return cudaGetLastError();
 }
 
@@ -766,7 +1061,7 @@ cudaError_t launch_type(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t s
   if (q.m <= 32) return launch_few<kType, 32>(q, p, stream);
   if (q.m <= 64) return launch_few<kType, 64>(q, p, stream);
   if (q.m <= 128) return launch_few<kType, 128>(q, p, stream);
-  return launch_pair<kType>(q, p, stream);
+  return q.scale_type == KS_SCALE_E8M0 ? launch_pair<kType, true>(q, p, stream) : launch_pair<kType, false>(q, p, stream);
 }
 
 }  // namespace
