@@ -282,6 +282,8 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
   __syncthreads();
   cluster_sync();  // both CTAs' barriers exist before either is used
   fence_after();
+  next_may_start();
+  wait_for_last();
   const uint32_t tmem = s_tmem;
   const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
   const uint32_t tiles = static_cast<uint32_t>(tiles_m) * tiles_n;  // (checked by the host)
@@ -577,6 +579,8 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
   __syncthreads();
   cluster_sync();  // both CTAs' barriers exist before either is used
   fence_after();
+  next_may_start();
+  wait_for_last();
   const uint32_t tmem = s_tmem;
   const int tiles_m = (p.m + kTile - 1) / kTile, tiles_n = (p.n + kTile - 1) / kTile;
   const uint32_t tiles = static_cast<uint32_t>(tiles_m) * tiles_n;
@@ -794,9 +798,10 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
                   const __grid_constant__ CUtensorMap map_b, int parts) {
   extern __shared__ unsigned char smem_raw[];
   constexpr int kS = kFewStages<kN>;
-  constexpr int kTmem = 2 * kN < 32 ? 32 : 2 * kN;
-  __shared__ __align__(8) Wide s_bar[2 * kS + 4];  // full, empty, accumulator full[2] and read out[2]
-  __shared__ __align__(16) float s_scale[4][2][kN];
+  constexpr int kAcc = kN <= 32 ? 4 : 2;  // accumulators
+  constexpr int kTmem = kAcc * kN;
+  __shared__ __align__(8) Wide s_bar[2 * kS + 2 * kAcc];  // full, empty, accumulator full and read out
+  __shared__ __align__(16) float s_scale[4][kAcc][kN];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
@@ -810,7 +815,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   auto bar_full = [&](int s) { return bar0 + 8u * s; };
   auto bar_empty = [&](int s) { return bar0 + 8u * (kS + s); };
   auto bar_acc = [&](int i) { return bar0 + 8u * (2 * kS + i); };
-  auto bar_read = [&](int i) { return bar0 + 8u * (2 * kS + 2 + i); };
+  auto bar_read = [&](int i) { return bar0 + 8u * (2 * kS + kAcc + i); };
 
   if (tid == 0) {
     s_fail = 0;
@@ -818,7 +823,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
       bar_init(bar_full(s), 1);
       bar_init(bar_empty(s), 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kAcc; ++i) {
       bar_init(bar_acc(i), 1);
       bar_init(bar_read(i), 4);
     }
@@ -831,6 +836,8 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   fence_before();
   __syncthreads();
   fence_after();
+  next_may_start();
+  wait_for_last();
   const uint32_t tmem = s_tmem;
   volatile int* v_fail = &s_fail;
   auto wait_ok = [&](uint32_t bar, uint32_t parity) {
@@ -860,8 +867,8 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     if (lane == 0) {
       constexpr uint32_t idesc = instr_desc(kScaleBlock, kN);
       for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-        const int s = it % kS, acc = it & 1;
-        if (!wait_ok(bar_read(acc), ((it >> 1) & 1u) ^ 1u) || !wait_ok(bar_full(s), (it / kS) & 1u)) break;
+        const int s = it % kS, acc = it % kAcc;
+        if (!wait_ok(bar_read(acc), ((it / kAcc) & 1u) ^ 1u) || !wait_ok(bar_full(s), (it / kS) & 1u)) break;
         fence_after();
         const uint64_t dw = operand_desc(sbase + s * kFewStageBytes<kN>);
         const uint64_t dx = operand_desc(sbase + s * kFewStageBytes<kN> + kOperandBytes);
@@ -891,13 +898,13 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     };
     if (kb0 < kb1) fetch(kb0);
     for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-      const int acc = it & 1;
+      const int acc = it % kAcc;
 #pragma unroll
       for (int e = 0; e < kEach; ++e)
         if (lane + 32 * e < kN) s_scale[w][acc][lane + 32 * e] = sa[e];
       __syncwarp();
       if (kb + 1 < kb1) fetch(kb + 1);
-      if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it >> 1) & 1u))) break;
+      if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it / kAcc) & 1u))) break;
       fence_after();
       const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_scale[w][acc]);
 #pragma unroll
@@ -1024,8 +1031,7 @@ cudaError_t launch_pair(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t s
   if (e != cudaSuccess) return e;
   const int64_t tiles = ((q.m + kTile - 1) / kTile) * ((q.n + kTile - 1) / kTile);
   if (tiles + kSms > UINT32_MAX) return cudaErrorInvalidConfiguration;
-  kernel<<<2 * static_cast<int>(std::min<int64_t>(tiles, kSms / 2)), kThreads, kBytes, stream>>>(p, ma, mb);
-  return cudaGetLastError();
+  return launch_following(kernel, dim3(2 * static_cast<unsigned>(std::min<int64_t>(tiles, kSms / 2))), kThreads, kBytes, 0, stream, p, ma, mb);
 }
 
 template <int kType, int kN>
@@ -1041,18 +1047,8 @@ cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t st
   // parts of K, so that the machine's CTAs have work each
   int parts = 1;
   while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * (kN <= 64 ? 2 : 1)) parts *= 2;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows));
-  cfg.blockDim = dim3(kFewThreads);
-  cfg.dynamicSmemBytes = kFewSmem<kN>;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(parts);
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, matmul_few_kernel<kType, kN>, p, ma, mb, parts);
+  return launch_following(&matmul_few_kernel<kType, kN>, dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows)), kFewThreads,
+                          kFewSmem<kN>, parts, stream, p, ma, mb, parts);
 }
 
 template <int kType>

@@ -6,6 +6,7 @@
 
 #include "ks_e4m3.cuh"
 #include "ks_internal.h"
+#include "ks_tcgen.cuh"
 
 namespace ks {
 namespace {
@@ -61,6 +62,8 @@ constexpr int kQuantThreads = 256;
 // A block of 1 x 128 belongs to the 16 or 32 lanes that its 16-byte pieces fill.
 template <typename T, bool kE8m0, bool kVec>
 __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const __grid_constant__ QuantArgs a) {
+  next_may_start();
+  wait_for_last();
   constexpr int kN = 16 / sizeof(T), kLanes = kScaleBlock / kN, kGroups = kQuantThreads / kLanes;
   const int64_t per_row = scale_blocks(a.cols), items = a.rows * per_row;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * kGroups + threadIdx.x / kLanes;
@@ -84,6 +87,8 @@ __global__ void __launch_bounds__(kQuantThreads) quantize_rows_kernel(const __gr
 // A block of 128 x 128 belongs to a CTA, 64 values a thread.
 template <typename T, bool kE8m0, bool kVec>
 __global__ void __launch_bounds__(kQuantThreads) quantize_tiles_kernel(const __grid_constant__ QuantArgs a) {
+  next_may_start();
+  wait_for_last();
   constexpr int kN = 16 / sizeof(T), kLanes = kScaleBlock / kN, kRows = kQuantThreads / kLanes;
   constexpr int kSteps = kScaleBlock / kRows;
   __shared__ float s_max[kQuantThreads / 32];
@@ -123,9 +128,8 @@ cudaError_t launch_quantize_as(const QuantArgs& a, int block_rows, cudaStream_t 
   const int64_t blocks = block_rows == 1 ? (a.rows * scale_blocks(a.cols) + kGroups - 1) / kGroups
                                          : scale_blocks(a.rows) * scale_blocks(a.cols);
   if (blocks > INT32_MAX) return cudaErrorInvalidConfiguration;
-  if (block_rows == 1) quantize_rows_kernel<T, kE8m0, kVec><<<static_cast<unsigned>(blocks), kQuantThreads, 0, stream>>>(a);
-  else quantize_tiles_kernel<T, kE8m0, kVec><<<static_cast<unsigned>(blocks), kQuantThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+  return launch_following(block_rows == 1 ? &quantize_rows_kernel<T, kE8m0, kVec> : &quantize_tiles_kernel<T, kE8m0, kVec>,
+                          dim3(static_cast<unsigned>(blocks)), kQuantThreads, 0, 0, stream, a);
 }
 
 template <typename T>

@@ -213,6 +213,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   __shared__ Shared<kWarps> s;
   extern __shared__ uint4 s_held[];  // [held_loads][threads]
   constexpr int V = 16 / static_cast<int>(sizeof(T));  // scores a load
+  next_may_start();
+  wait_for_last();
   const int rank = ctas == 1 ? 0 : static_cast<int>(blockIdx.x) % ctas;
   const int64_t p = blockIdx.x / ctas;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -743,18 +745,8 @@ cudaError_t launch_as(const SampleArgs& a, int ctas, int held_loads, cudaStream_
   cudaError_t e = ensure_dynamic_smem(kernel, kHeldLoads * kThreads * 16);
   if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.p * ctas));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = static_cast<size_t>(held_loads) * kThreads * 16;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(ctas);
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, sample_kernel<T, kThreads>, a, ctas, held_loads);
+  return launch_following(&sample_kernel<T, kThreads>, dim3(static_cast<unsigned>(a.p * ctas)), kThreads,
+                          static_cast<size_t>(held_loads) * kThreads * 16, ctas, stream, a, ctas, held_loads);
 }
 
 constexpr int kSmall = 256, kLarge = 512;  // threads of a CTA
