@@ -9,6 +9,10 @@
 // place in it. A histogram over the distance to the best score narrows it down to one bin, in which some hundred candidates
 // lie; they are sorted. Bins that hold more are narrowed down further by the bits of (score, index).
 //
+// The sums of weights that top-p's histogram needs are first estimated in 32 bits; one pass with the weights themselves then
+// sums up what lies surely in front of the cut and lists the candidates of the few bins around it, which are sorted. Where the
+// estimate was not good enough the exact histogram is made.
+//
 // A short front (top-k of some hundred) needs no histogram: the k-th largest of the maxima of 128 parts of the row bounds the
 // k-th score from below, so that little more than k candidates are listed, sorted, cut, and drawn from in the list.
 //
@@ -122,8 +126,8 @@ struct Shared {
   Wide best;
   float least[kWarps], min, bound;
   alignas(16) float part[kParts];
-  Wide share, before, total, cut;
-  int bin;
+  Wide share, before, total, cut, front;
+  int bin, first_bin, last_bin;
   unsigned listed;
 };
 
@@ -640,8 +644,171 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
       return;
     }
   };
+  Wide* ends = s.list;   // sums of the stretches of this CTA, then up to their ends
+  bool summed = false;   // they are there
+  // The cut of top-p by an estimate; false: it did not serve.
+  auto estimated_cut = [&](double part) KS_INLINE -> bool {
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.low[i] = s.high[i] = 0;
+    if (threadIdx.x == 0) s.listed = 0;
+    __syncthreads();
+    const float octaves = 1.4426950408889634f / set.temperature;
+    each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float w;  // (the relative error of 53 octaves in fp32 is below 2^-18)
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"((y[v] - r.best) * octaves));
+        const unsigned add = y[v] == r.best ? 0x80000000u : __float2uint_rn(w * 2147483648.0f);
+        if (add == 0 || !inside(i + v, y[v])) continue;
+        const int d = bin_of(r, y[v]);
+        const unsigned was = atomicAdd(&s.low[d], add);
+        if (was + add < was) atomicAdd(&s.high[d], 1u);
+      }
+    });
+    meet(ctas);
+    Wide own = 0, share;
+    for (int i = threadIdx.x; i < mine; i += kThreads) {
+      Wide b = 0;
+      if (ctas == 1) {
+        b = bin_sum(i);
+      } else {
+        for (int o = 0; o < ctas; ++o)
+          b += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
+        s.merged[i] = b;
+      }
+      own += b;
+    }
+    block_scan(own, s.warp, share);
+    if (threadIdx.x == 0) s.share = share;
+    meet(ctas);
+    Wide before = 0, all = 0;
+    for (int o = 0; o < ctas; ++o) {
+      const Wide t = *of_rank(&s.share, o, ctas);
+      if (o < rank) before += t;
+      all += t;
+    }
+    // the bins in which the sum reaches a little less and a little more than the part
+    const double goal = part * static_cast<double>(all);
+    const Wide least = static_cast<Wide>(goal * (1.0 - 1.0 / 8192)), most = min(all, static_cast<Wide>(goal * (1.0 + 1.0 / 8192)) + 1);
+    if (threadIdx.x == 0) s.first_bin = s.last_bin = -1;
+    Wide mine_sum = 0, total;
+    for (int q = 0; q < per; ++q)
+      if (static_cast<int>(threadIdx.x) * per + q < mine) mine_sum += bin_sum(threadIdx.x * per + q);
+    Wide b = block_scan(mine_sum, s.warp, total) + before;
+    for (int q = 0; q < per && static_cast<int>(threadIdx.x) * per + q < mine; ++q) {
+      const int i = threadIdx.x * per + q;
+      const Wide e = b + bin_sum(i);
+      if (b <= least && e > least) s.first_bin = rank * mine + i;
+      if (b < most && e >= most) s.last_bin = rank * mine + i;
+      b = e;
+    }
+    meet(ctas);
+    int first_bin = -1, last_bin = -1;
+    for (int o = 0; o < ctas; ++o) {
+      first_bin = max(first_bin, *of_rank(&s.first_bin, o, ctas));
+      last_bin = max(last_bin, *of_rank(&s.last_bin, o, ctas));
+    }
+    if (first_bin < 0 || last_bin < 0) {  // (all threads find the same)
+      meet(ctas);
+      return false;
+    }
+    // the weights: of all, of what lies in front of those bins (by stretches what min-p lets stay), and who lies in them
+    unsigned* n_list = of_rank(&s.listed, 0, ctas);
+    Wide* list = of_rank(&s.list[0], 0, ctas);
+    ends = reinterpret_cast<Wide*>(s.low);
+    Wide sum = 0, front = 0;
+    for (int tile = 0; tile < tiles; ++tile) {
+      Wide stretch = 0;
+      uint32_t at = place(tile, warp, 0);
+      const uint32_t lane0 = at - lane * V;
+      const int steps = lane0 >= last ? 0 : min(loads, static_cast<int>((last - lane0 + 32 * V - 1) / (32 * V)));
+      uint4 next = make_uint4(0, 0, 0, 0);
+      if (steps > 0) next = get(at, warp, 0);
+#pragma unroll 1
+      for (int q = 0; q < steps; ++q, at += 32 * V) {
+        float y[V];
+        unpack(next, y, T{});
+        if (q + 1 < steps) next = get(at + 32 * V, warp, q + 1);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const double exact = scaled_weight(r, s.table, y[v]);
+          const bool in = inside(at + v, y[v]) && !(r.best - y[v] > r.reach);
+          const Wide w = in ? whole(exact) : 0;
+          const int bin = bin_of(r, y[v]);
+          sum += w;
+          if (bin < first_bin) {
+            front += w;
+            if (exact >= r.least) stretch += w;
+          } else if (bin <= last_bin && w > 0) {
+            const unsigned to = atomicAdd(n_list, 1u);
+            if (to < kList) list[to] = key_of(at + v, y[v]);
+          }
+        }
+      }
+      stretch = warp_sum(stretch);
+      if (lane == 0) ends[tile * kWarps + warp] = stretch;
+    }
+    Wide block_sum, block_front;
+    block_scan(sum, s.warp, block_sum);
+    block_scan(front, s.warp, block_front);
+    if (threadIdx.x == 0) {
+      s.share = block_sum;
+      s.front = block_front;
+      s.cut = 0;
+    }
+    meet(ctas);
+    const unsigned listed = *n_list;
+    if (rank == 0) {
+      all = front = 0;
+      for (int o = 0; o < ctas; ++o) {
+        all += *of_rank(&s.share, o, ctas);
+        front += *of_rank(&s.front, o, ctas);
+      }
+      const Wide target = max(1ull, static_cast<Wide>(ceil(part * static_cast<double>(all))));
+      if (listed <= kList && front < target) {
+        sort_list<kThreads>(s.list, static_cast<int>(listed));
+        constexpr int kEach = kList / kThreads;
+        Wide w[kEach];
+        sum = 0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+          const unsigned i = threadIdx.x * kEach + q;
+          w[q] = i >= listed ? 0 : weight(key_score(s.list[i]));
+          sum += w[q];
+        }
+        Wide e = block_scan(sum, s.warp, total) + front;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+          if (e < target && e + w[q] >= target) s.cut = s.list[threadIdx.x * kEach + q];
+          e += w[q];
+        }
+      }
+    }
+    meet(ctas);
+    const Wide cut = *of_rank(&s.cut, 0, ctas);
+    if (cut == 0) {
+      ends = s.list;
+      meet(ctas);  // (it is read)
+      return false;
+    }
+    cut_score = key_score(cut);
+    cut_at = static_cast<unsigned>(key_index(cut));
+    // of the candidates listed those that stay belong to stretches too
+    for (unsigned i = threadIdx.x; i < listed; i += kThreads) {
+      const Wide key = list[i];
+      const uint32_t at = static_cast<uint32_t>(key_index(key)) + shift;
+      if (key < cut || at < first || at >= last) continue;
+      const double exact = scaled_weight(r, s.table, key_score(key));
+      if (exact >= r.least) atomicAdd(&ends[(at - first) / (32 * V) / loads], whole(exact));
+    }
+    __syncthreads();
+    summed = true;
+    return true;
+  };
   if (!greedy && set.top_k > 0) find_cut(std::true_type{}, static_cast<Wide>(set.top_k), 0.0);
-  if (!greedy && set.top_p < 1.0f) find_cut(std::false_type{}, 0, fmax(static_cast<double>(set.top_p), 0.0));
+  if (!greedy && set.top_p < 1.0f) {
+    const double part = fmax(static_cast<double>(set.top_p), 0.0);
+    if (!estimated_cut(part)) find_cut(std::false_type{}, 0, part);
+  }
 
   // ---- the sum of what stays, then the draws, in the order of the indices ----
   auto stays = [&](uint32_t i, float y) KS_INLINE -> Wide {
@@ -650,7 +817,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   };
   const int entries = tiles * kWarps;  // a tile's parts by warp, in the order of the indices
   __syncthreads();  // (the list is read)
-  for (int tile = 0; tile < tiles; ++tile) {
+  for (int tile = 0; tile < tiles && !summed; ++tile) {
     Wide own = 0;
     uint32_t at = place(tile, warp, 0);
     const uint32_t lane0 = at - lane * V;
@@ -671,17 +838,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
       for (int v = 0; v < V; ++v) own += stays(at + v, y[v]);
     }
     own = warp_sum(own);
-    if (lane == 0) s.list[tile * kWarps + warp] = own;
+    if (lane == 0) ends[tile * kWarps + warp] = own;
   }
   __syncthreads();
   {  // sums up to an entry's end
     const int per_thread = (entries + kThreads - 1) / kThreads;
     Wide own = 0, total;
     for (int e = 0; e < per_thread; ++e)
-      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) own += s.list[threadIdx.x * per_thread + e];
+      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) own += ends[threadIdx.x * per_thread + e];
     Wide upto = block_scan(own, s.warp, total);
     for (int e = 0; e < per_thread; ++e)
-      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) s.list[threadIdx.x * per_thread + e] = upto += s.list[threadIdx.x * per_thread + e];
+      if (static_cast<int>(threadIdx.x) * per_thread + e < entries) ends[threadIdx.x * per_thread + e] = upto += ends[threadIdx.x * per_thread + e];
     if (threadIdx.x == 0) s.total = total;
   }
   meet(ctas);
@@ -700,10 +867,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     int lo = 0, hi = entries - 1;  // the first entry whose end is behind the target
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
-      if (s.list[mid] > target) hi = mid;
+      if (ends[mid] > target) hi = mid;
       else lo = mid + 1;
     }
-    target -= lo > 0 ? s.list[lo - 1] : 0;
+    target -= lo > 0 ? ends[lo - 1] : 0;
     const int tile = lo / kWarps, w_slot = lo % kWarps;
 #pragma unroll 1
     for (int q = 0; q < loads; ++q) {
