@@ -83,8 +83,9 @@ __device__ __forceinline__ Wide whole(double w) {
   return static_cast<Wide>(__double_as_longlong(w + 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
 }
 
+// (adding 2^23 rounds to a whole number in the low bits)
 __device__ __forceinline__ int bin_of(const Row& r, float x) {
-  return static_cast<int>(fminf((r.best - x) * r.bins, static_cast<float>(kBins - 1)));
+  return static_cast<int>(__float_as_uint(fminf((r.best - x) * r.bins, static_cast<float>(kBins - 1)) + 8388608.0f) & (kBins - 1));
 }
 
 __device__ __forceinline__ Wide warp_scan(Wide v, int lane) {  // inclusive
@@ -168,28 +169,28 @@ __device__ __forceinline__ void sort_list(Wide* list, int n) {
 
 // The scores of one load, with what is no number as -inf and of the two zeros one.
 __device__ __forceinline__ float normal(float y) { return fmaxf(y + 0.0f, __int_as_float(0xFF800000)); }
-__device__ __forceinline__ void unpack(const uint4& w, float (&y)[4], float) {
-  y[0] = normal(__uint_as_float(w.x));
-  y[1] = normal(__uint_as_float(w.y));
-  y[2] = normal(__uint_as_float(w.z));
-  y[3] = normal(__uint_as_float(w.w));
-}
-__device__ __forceinline__ void unpack(const uint4& w, float (&y)[8], __nv_bfloat16) {
+template <typename T, int V>
+__device__ __forceinline__ void unpack_as_is(const uint4& w, float (&y)[V]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    y[2 * i] = normal(__uint_as_float(u[i] << 16));
-    y[2 * i + 1] = normal(__uint_as_float(u[i] & 0xFFFF0000u));
+    if constexpr (V == 4) {
+      y[i] = __uint_as_float(u[i]);
+    } else if constexpr (is_bf16<T>) {
+      y[2 * i] = __uint_as_float(u[i] << 16);
+      y[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    } else {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+      y[2 * i] = f.x;
+      y[2 * i + 1] = f.y;
+    }
   }
 }
-__device__ __forceinline__ void unpack(const uint4& w, float (&y)[8], __half) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+template <typename T, int V>
+__device__ __forceinline__ void unpack(const uint4& w, float (&y)[V]) {
+  unpack_as_is<T, V>(w, y);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
-    y[2 * i] = normal(f.x);
-    y[2 * i + 1] = normal(f.y);
-  }
+  for (int v = 0; v < V; ++v) y[v] = normal(y[v]);
 }
 // The load of scores at a place of which some lie outside [shift, last): those as -inf.
 template <typename T>
@@ -256,8 +257,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   };
   auto get = [&](uint32_t at, int w, int q) KS_INLINE { return held ? s_held[q * kThreads + w * 32 + lane] : fetch(at); };
   auto key_of = [&](uint32_t at, float y) KS_INLINE { return make_key(y, static_cast<int>(at - shift)); };
-  // f(place, scores) for all loads of this thread
-  auto each = [&](auto f) KS_INLINE {
+  // f(place, scores) for all loads of this thread, as they are or with what is no number as -inf
+  auto each_load = [&](auto as_is, auto f) KS_INLINE {
     for (int tile = 0; tile < tiles; ++tile) {
       uint32_t at = place(tile, warp, 0);
       const uint32_t lane0 = at - lane * V;
@@ -267,12 +268,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll 1
       for (int q = 0; q < mine; ++q, at += 32 * V) {
         float y[V];
-        unpack(next, y, T{});
+        if constexpr (decltype(as_is)::value) unpack_as_is<T, V>(next, y);
+        else unpack<T, V>(next, y);
         if (q + 1 < mine) next = get(at + 32 * V, warp, q + 1);  // on its way while these are worked on
         f(at, y);
       }
     }
   };
+  auto each = [&](auto f) KS_INLINE { each_load(std::false_type{}, f); };
 
   // ---- the best candidate, and the least score that is a number ----
   float top = none, low = __int_as_float(0x7F800000);
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (q0 + q >= loads) break;
         if (held) s_held[(q0 + q) * kThreads + threadIdx.x] = w[q];
         float y[V];
-        unpack(w[q], y, T{});
+        unpack<T, V>(w[q], y);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           top = fmaxf(top, y[v]);
@@ -652,17 +655,30 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (threadIdx.x == 0) s.listed = 0;
     __syncthreads();
     const float octaves = 1.4426950408889634f / set.temperature;
-    each([&](uint32_t i, const float (&y)[V]) KS_INLINE {
+    const bool cuts = cut_score > none;  // an earlier cut leaves some
+    each_load(std::true_type{}, [&](uint32_t i, const float (&y)[V]) KS_INLINE {
+      unsigned add[V], d[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float w;  // (the relative error of 53 octaves in fp32 is below 2^-18)
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"((y[v] - r.best) * octaves));
-        const unsigned add = y[v] == r.best ? 0x80000000u : __float2uint_rn(w * 2147483648.0f);
-        if (add == 0 || !inside(i + v, y[v])) continue;
-        const int d = bin_of(r, y[v]);
-        const unsigned was = atomicAdd(&s.low[d], add);
-        if (was + add < was) atomicAdd(&s.high[d], 1u);
+        // The weight times 2^30 (with 2^22, which needs no conversion, 16-bit scores that share a value are all rounded the same
+        // way, and the estimate failed for one row in 20). The relative error of 53 octaves in fp32 is below 2^-18. What is no
+        // number, or -inf, adds 0.
+        const float below = y[v] - r.best;
+        float w;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(below * octaves));
+        add[v] = __float2uint_rn(w * 1073741824.0f);
+        d[v] = __float_as_uint(fminf(-below * r.bins, static_cast<float>(kBins - 1)) + 8388608.0f) & (kBins - 1);
       }
+      if (cuts)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (!inside(i + v, y[v])) add[v] = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (add[v] > 0) {
+          const unsigned was = atomicAdd(&s.low[d[v]], add[v]);
+          if (was + add[v] < was) atomicAdd(&s.high[d[v]], 1u);
+        }
     });
     meet(ctas);
     Wide own = 0, share;
@@ -715,6 +731,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     unsigned* n_list = of_rank(&s.listed, 0, ctas);
     Wide* list = of_rank(&s.list[0], 0, ctas);
     ends = reinterpret_cast<Wide*>(s.low);
+    const bool least_counts = r.least > 0.0;
     Wide sum = 0, front = 0;
     for (int tile = 0; tile < tiles; ++tile) {
       Wide stretch = 0;
@@ -726,24 +743,26 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll 1
       for (int q = 0; q < steps; ++q, at += 32 * V) {
         float y[V];
-        unpack(next, y, T{});
+        unpack_as_is<T, V>(next, y);
         if (q + 1 < steps) next = get(at + 32 * V, warp, q + 1);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const double exact = scaled_weight(r, s.table, y[v]);
-          const bool in = inside(at + v, y[v]) && !(r.best - y[v] > r.reach);
+          bool in = r.best - y[v] <= r.reach;  // (not so of what is no number)
+          if (cuts) in = in && inside(at + v, y[v]);
           const Wide w = in ? whole(exact) : 0;
           const int bin = bin_of(r, y[v]);
           sum += w;
           if (bin < first_bin) {
-            front += w;
-            if (exact >= r.least) stretch += w;
+            if (!least_counts) stretch += w;
+            else front += w, stretch += exact >= r.least ? w : 0;
           } else if (bin <= last_bin && w > 0) {
             const unsigned to = atomicAdd(n_list, 1u);
-            if (to < kList) list[to] = key_of(at + v, y[v]);
+            if (to < kList) list[to] = key_of(at + v, normal(y[v]));
           }
         }
       }
+      if (!least_counts) front += stretch;
       stretch = warp_sum(stretch);
       if (lane == 0) ends[tile * kWarps + warp] = stretch;
     }
@@ -807,7 +826,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   if (!greedy && set.top_k > 0) find_cut(std::true_type{}, static_cast<Wide>(set.top_k), 0.0);
   if (!greedy && set.top_p < 1.0f) {
     const double part = fmax(static_cast<double>(set.top_p), 0.0);
-    if (!estimated_cut(part)) find_cut(std::false_type{}, 0, part);
+    // (an infinite score's distance to itself is no number: the estimate is for others)
+    if (!(r.best < __int_as_float(0x7F800000)) || !estimated_cut(part)) find_cut(std::false_type{}, 0, part);
   }
 
   // ---- the sum of what stays, then the draws, in the order of the indices ----
@@ -827,7 +847,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll 1
     for (int q = 0; q < mine; ++q, at += 32 * V) {
       float y[V];
-      unpack(next, y, T{});
+      unpack<T, V>(next, y);
       if (q + 1 < mine) next = get(at + 32 * V, warp, q + 1);
       // (where a cut leaves nothing of a warp's scores there is nothing to compute)
       float most = y[0];
@@ -876,7 +896,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     for (int q = 0; q < loads; ++q) {
       float y[V];
       const uint32_t i0 = place(tile, w_slot, q);
-      unpack(get(i0, w_slot, q), y, T{});
+      unpack<T, V>(get(i0, w_slot, q), y);
       Wide w[V], own = 0;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
