@@ -78,7 +78,7 @@ struct MatmulArgs {
   int relu;
   void* d;
   int64_t ldd;
-  int wide_rows;  // rows of d begin on 32-byte boundaries
+  int row_bytes;  // rows of d begin on boundaries of 32 bytes, 16, or (0) less
   void* d_scale;
   int wait_limit, starve;
   int* status;
@@ -151,7 +151,7 @@ struct PairShared {  // behind the stages
   float b_scale[2][2][kChunk];
   float bias[2][kTile];
   Tile tile[2];
-  float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 32-byte boundaries
+  float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 16-byte boundaries
   float amax[2][16][32];  // of a warp's rows, for the one that has the block's other half
 };
 constexpr int kSmem = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(PairShared));
@@ -201,7 +201,9 @@ template <int kType>
 __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, const float (&sum)[kCols], bool odd, float* s_store) {
   const int lane = threadIdx.x & 31;
   constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
-  if (p.wide_rows && n0 + kCols <= p.n) {
+  // (rows on boundaries of 16 bytes, 20,357 x 4,340 x 1,230: fp32 322 us by threads that write their own row, 235 through shared
+  // memory; bf16 197 and 201. Of 32 bytes, n = 4,352: 183 and 174, 151 and 201.)
+  if ((kType == KS_F32 ? p.row_bytes == 32 : p.row_bytes > 0) && n0 + kCols <= p.n) {
     char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row) * p.ldd + n0) * kBytes<kType>;
 #pragma unroll
     for (int g = 0; g < kCols / (8 * kPer); ++g) {  // 32 bytes at a time: a sector of the thread's row
@@ -212,10 +214,15 @@ __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0
         if (kType == KS_E4M3 && !odd) w[i] = e4m3_pair_finite(v[0], v[1]) | (e4m3_pair_finite(v[2], v[3]) << 16);
         else w[i] = pack<kType>(v);
       }
-      if (row < p.m)
+      if (row >= p.m) continue;
+      if (p.row_bytes == 16) {
+        reinterpret_cast<uint4*>(out)[2 * g] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(out)[2 * g + 1] = make_uint4(w[4], w[5], w[6], w[7]);
+      } else {
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(out + 32 * g), "r"(w[0]), "r"(w[1]),
                      "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
                      : "memory");
+      }
     }
     return;
   }
@@ -787,21 +794,22 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
 constexpr int kFewThreads = 256;  // warp 0 loads, warp 1 issues MMAs, warps 4..7 are the epilogue
 constexpr int kRedPitch = kScaleBlock + 4;
 
-template <int kN> constexpr int kFewStages = kN <= 64 ? 4 : 5;
+constexpr int kFewStages = 4;
 template <int kN> constexpr int kFewStageBytes = kOperandBytes + kN * kScaleBlock;
-template <int kN> constexpr int kFewSmem = 1024 + kFewStages<kN> * kFewStageBytes<kN>;
-static_assert(kFewSmem<16> - 1024 >= 16 * kRedPitch * 4 && kFewSmem<128> - 1024 >= 128 * kRedPitch * 4, "the sums fit the stages");
+template <int kN> constexpr int kFewSmem = 1024 + kFewStages * kFewStageBytes<kN>;
+static_assert(kFewSmem<16> - 1024 >= 16 * kRedPitch * 4 && kFewSmem<64> - 1024 >= 64 * kRedPitch * 4, "the sums fit the stages");
 
 template <int kType, int kN>
-__global__ void __launch_bounds__(kFewThreads, kN <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(kFewThreads, 2)
 matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ CUtensorMap map_a,
                   const __grid_constant__ CUtensorMap map_b, int parts) {
   extern __shared__ unsigned char smem_raw[];
-  constexpr int kS = kFewStages<kN>;
-  constexpr int kAcc = kN <= 32 ? 4 : 2;  // accumulators
+  constexpr int kS = kFewStages;
+  constexpr int kAcc = 4;  // accumulators
   constexpr int kTmem = kAcc * kN;
-  __shared__ __align__(8) Wide s_bar[2 * kS + 2 * kAcc];  // full, empty, accumulator full and read out
-  __shared__ __align__(16) float s_scale[4][kAcc][kN];
+  constexpr int kChunk = 8;  // blocks of K whose scales are brought together
+  __shared__ __align__(8) Wide s_bar[2 * kS + 2 * kAcc + 4];  // full, empty, accumulator full and read out, scales full[2] and used[2]
+  __shared__ __align__(16) float s_scale[2][kChunk][kN];
   __shared__ uint32_t s_tmem;
   __shared__ int s_fail;
 
@@ -816,6 +824,8 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   auto bar_empty = [&](int s) { return bar0 + 8u * (kS + s); };
   auto bar_acc = [&](int i) { return bar0 + 8u * (2 * kS + i); };
   auto bar_read = [&](int i) { return bar0 + 8u * (2 * kS + kAcc + i); };
+  auto bar_scale = [&](int i) { return bar0 + 8u * (2 * kS + 2 * kAcc + i); };
+  auto bar_used = [&](int i) { return bar0 + 8u * (2 * kS + 2 * kAcc + 2 + i); };
 
   if (tid == 0) {
     s_fail = 0;
@@ -826,6 +836,10 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     for (int i = 0; i < kAcc; ++i) {
       bar_init(bar_acc(i), 1);
       bar_init(bar_read(i), 4);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(bar_scale(i), 2);
+      bar_init(bar_used(i), 4);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -879,34 +893,37 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
       }
     }
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (warp < 4) {
+    // The scales' products: threads by row and by stretches of a chunk, once for the four warps that use them (each of which
+    // fetching its own took 28 us where this takes 20: 64 rows by 8,192 x 8,192, fp32 scales)
+    constexpr int kOf = kN * kChunk / 64;  // blocks of a thread
+    const int t = threadIdx.x - 64, r = t % kN, first = t / kN * kOf, m = m0 + r;
+    const int64_t sa_at = static_cast<int64_t>(m < p.m ? m : 0) * p.kblocks, sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
+    for (int kb = kb0, it = 0; kb < kb1; kb += kChunk, ++it) {
+      float v[kOf];
+#pragma unroll
+      for (int k = 0; k < kOf; ++k)
+        v[k] = m < p.m && kb + first + k < kb1 ? scale_value(p.a_scale, sa_at + kb + first + k, p.scale_type) *
+                                                     scale_value(p.b_scale, sb_at + kb + first + k, p.scale_type) : 0.0f;
+      if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_used(it & 1), ((it >> 1) & 1u) ^ 1u))) break;
+#pragma unroll
+      for (int k = 0; k < kOf; ++k) s_scale[it & 1][first + k][r] = v[k];
+      __syncwarp();
+      if (lane == 0) bar_arrive(bar_scale(it & 1));
+    }
+  } else {
     const int w = warp - 4;
     const uint32_t tmem_mine = tmem + (static_cast<uint32_t>(w * 32) << 16);
-    constexpr int kLoad = kN < 32 ? kN : 32, kEach = (kN + 31) / 32;
+    constexpr int kLoad = kN < 32 ? kN : 32;
     Wide sum[kN / 2];
 #pragma unroll
     for (int q = 0; q < kN / 2; ++q) sum[q] = 0;
-    float sa[kEach];
-    const int64_t sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
-    auto fetch = [&](int kb) {
-      const float sb = scale_value(p.b_scale, sb_at + kb, p.scale_type);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        const int m = m0 + lane + 32 * e;
-        sa[e] = m < p.m && lane + 32 * e < kN ? scale_value(p.a_scale, static_cast<int64_t>(m) * p.kblocks + kb, p.scale_type) * sb : 0.0f;
-      }
-    };
-    if (kb0 < kb1) fetch(kb0);
     for (int kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-      const int acc = it % kAcc;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (lane + 32 * e < kN) s_scale[w][acc][lane + 32 * e] = sa[e];
-      __syncwarp();
-      if (kb + 1 < kb1) fetch(kb + 1);
+      const int acc = it % kAcc, buf = (it / kChunk) & 1;
+      if (it % kChunk == 0 && !__all_sync(0xFFFFFFFFu, wait_ok(bar_scale(buf), (it / kChunk / 2) & 1u))) break;
       if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_acc(acc), (it / kAcc) & 1u))) break;
       fence_after();
-      const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_scale[w][acc]);
+      const ulonglong2* sc = reinterpret_cast<const ulonglong2*>(s_scale[buf][it % kChunk]);
 #pragma unroll
       for (int c = 0; c < kN; c += kLoad) {
         uint32_t r[32];
@@ -931,7 +948,10 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
       }
       fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(bar_read(acc));
+      if (lane == 0) {
+        bar_arrive(bar_read(acc));
+        if (it % kChunk == kChunk - 1) bar_arrive(bar_used(buf));
+      }
     }
     // (the last accumulator is read: every copy has arrived and every MMA is done)
     asm volatile("barrier.cta.sync 1, 128;" ::: "memory");
@@ -977,7 +997,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] *= inv;
       }
-      if (p.wide_rows && n + 4 <= p.n) {
+      if (p.row_bytes && n + 4 <= p.n) {
         char* out = static_cast<char*>(p.d) + (row * p.ldd + n) * kBytes<kType>;
         if (kType == KS_F32) *reinterpret_cast<float4*>(out) = make_float4(v[0], v[1], v[2], v[3]);
         else if (kType == KS_E4M3) *reinterpret_cast<uint32_t*>(out) = pack<kType>(v);
@@ -1046,17 +1066,17 @@ cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t st
   if (tiles * 8 > INT32_MAX || rows > 65535) return cudaErrorInvalidConfiguration;
   // parts of K, so that the machine's CTAs have work each
   int parts = 1;
-  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * (kN <= 64 ? 2 : 1)) parts *= 2;
+  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * 2) parts *= 2;
   return launch_following(&matmul_few_kernel<kType, kN>, dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows)), kFewThreads,
                           kFewSmem<kN>, parts, stream, p, ma, mb, parts);
 }
 
 template <int kType>
 cudaError_t launch_type(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
+  // (65 and 128 rows by 8,192 x 8,192: 41 and 47 us by columns of 128, 34 and 35 by pairs; 64 rows 24 and 34)
   if (q.m <= 16) return launch_few<kType, 16>(q, p, stream);
   if (q.m <= 32) return launch_few<kType, 32>(q, p, stream);
   if (q.m <= 64) return launch_few<kType, 64>(q, p, stream);
-  if (q.m <= 128) return launch_few<kType, 128>(q, p, stream);
   return q.scale_type == KS_SCALE_E8M0 ? launch_pair<kType, true>(q, p, stream) : launch_pair<kType, false>(q, p, stream);
 }
 
@@ -1075,7 +1095,8 @@ cudaError_t launch_matmul_e4m3(const MatmulE4m3& q, int* status, cudaStream_t st
   p.relu = q.relu;
   p.d = q.d;
   p.ldd = q.ldd;
-  p.wide_rows = reinterpret_cast<uintptr_t>(q.d) % 32 == 0 && (q.m == 1 || q.ldd * bytes % 32 == 0);
+  const uintptr_t ends = reinterpret_cast<uintptr_t>(q.d) | (q.m == 1 ? 0 : static_cast<uintptr_t>(q.ldd * bytes));
+  p.row_bytes = ends % 32 == 0 ? 32 : ends % 16 == 0 ? 16 : 0;
   p.d_scale = q.d_scale;
   p.wait_limit = wait->limit > 0 ? wait->limit : kMlpWaitLimit;
   p.starve = wait->starve;

@@ -244,3 +244,24 @@ def test_binding_refuses(ctx):
         ctx.quantize_e4m3(torch.zeros(4, 4, device=DEV), block_rows=2)
     with pytest.raises(ks.KsError):  # rows that do not begin on 16-byte boundaries
         ctx.matmul_e4m3(torch.zeros(4, 20, device=DEV).to(torch.float8_e4m3fn), sa, torch.zeros(8, 20, device=DEV).to(torch.float8_e4m3fn), sb)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("m", [40, 300])
+@pytest.mark.parametrize("ldd", [256, 264, 260, 257, 258])
+def test_matmul_rows_that_begin_anywhere(ctx, m, ldd, dtype, scale):
+    """Results whose rows begin on boundaries of 32 bytes, of 16 and of less, at the buffer's start and inside it."""
+    n, k = 256, 200
+    (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, n, k, scale, 3)
+    top = float(2.0 ** np.ceil(np.log2(np.abs(lowbit.matmul(av, sav, bv, sbv)[0]).max())))
+    sa = (sa.float() / top).to(sa.dtype)  # the sums fit 16 bits
+    want, mag = lowbit.matmul(av, lowbit.as_float64(sa), bv, sbv)
+    for start in (0, 8, 3):
+        flat = torch.full((m * ldd + 16,), 7.0, dtype=dtype, device=DEV)
+        out = flat[start:start + m * ldd].view(m, ldd)[:, :n]
+        ctx.matmul_e4m3(a, sa, b, sb, out_dtype=dtype, out=out)
+        assert (np.abs(lowbit.as_float64(out) - want) <= off_by(k, mag, want, dtype)).all()
+        left = flat.clone()
+        left[start:start + m * ldd].view(m, ldd)[:, :n] = 7.0
+        assert bool((left == 7).all())
