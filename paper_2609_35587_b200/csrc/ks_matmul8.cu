@@ -143,6 +143,22 @@ constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kChunk = 8;  // blocks of K whose scales are brought together
 constexpr int kCols = 64;  // of an epilogue warp
 constexpr int kStorePitch = 9;
+// The next stage of the warp that issues MMAs: its barriers, and the low half of its operands' descriptor.
+__device__ __forceinline__ uint32_t operand_low(uint32_t saddr) { return static_cast<uint32_t>(operand_desc(saddr)); }
+__device__ __forceinline__ uint64_t operand_at(uint32_t low) { return (operand_desc(0) & 0xFFFFFFFF00000000ull) | low; }
+struct Ring {
+  uint32_t full, empty, low, parity;
+  int stage;
+  __device__ __forceinline__ void next() {
+    const bool wraps = ++stage == kStages;
+    stage = wraps ? 0 : stage;
+    parity ^= wraps ? 1u : 0u;
+    full += wraps ? 8u - 8u * kStages : 8u;
+    empty += wraps ? 8u - 8u * kStages : 8u;
+    low += wraps ? (kStageBytes >> 4) - (kStageBytes >> 4) * kStages : (kStageBytes >> 4);
+  }
+};
+
 struct Tile {
   int m, n;
 };
@@ -341,29 +357,25 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
     } else if (warp == 1) {
       if (rank == 0) {
         const bool lead = elect_one();
-        uint32_t s = 0, parity = 0, acc = 0, parity_acc = 1;
+        // (what a block of K takes this warp is a chain: the next stage, accumulator and barriers are kept, not computed)
+        Ring ring{bar_full(0), bar_empty(0), operand_low(sbase), 0, 0};
+        uint32_t acc = 0, parity_acc = 1;
         bool ok = true;
         constexpr uint32_t idesc = instr_desc(kTile, kTile);
-        const uint64_t desc0 = operand_desc(sbase);
         for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
           for (int kb = 0; kb < p.kblocks; ++kb) {
-            if (!(ok = wait_ok(bar_read(acc), parity_acc) && wait_ok(bar_full(s), parity))) break;
+            if (!(ok = wait_ok(bar_read(0) + 8u * acc, parity_acc) && wait_ok(ring.full, ring.parity))) break;
             fence_after();
-            const uint64_t da = desc0 + s * (kStageBytes >> 4), db = da + (kOperandBytes >> 4);
-            const uint32_t d = tmem + acc * kTile;
             if (lead) {
 #pragma unroll
               for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
-                mma<1>(d, da + 2u * k, db + 2u * k, idesc, k > 0);
-              commit_pair(bar_empty(s));
-              commit_pair(bar_acc(acc));
+                mma<1>(tmem + acc * kTile, operand_at(ring.low + 2u * k), operand_at(ring.low + (kOperandBytes >> 4) + 2u * k), idesc, k > 0);
+              commit_pair(ring.empty);
+              commit_pair(bar_acc(0) + 8u * acc);
             }
-            if (++s == kStages) {
-              s = 0;
-              parity ^= 1u;
-            }
+            ring.next();
+            parity_acc ^= acc;  // (after the second of the two)
             acc ^= 1u;
-            if (acc == 0) parity_acc ^= 1u;
           }
         }
       }
@@ -632,45 +644,43 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
     } else if (warp == 1) {
       if (rank == 0) {
         const bool lead = elect_one();
-        uint32_t s = 0, parity = 0, parity_acc = 1, buf = 0, parity_scale = 0;
+        Ring ring{bar_full(0), bar_empty(0), operand_low(sbase), 0, 0};
+        uint32_t parity_acc = 1, buf = 0, parity_scale = 0;
         bool ok = true;
-        const uint64_t desc0 = operand_desc(sbase);
         const uint32_t scale0 = smem_addr(&sh.scale[0][0]);
         for (uint32_t t = pair; t < tiles && ok; t += n_pairs) {
-          for (int kb = 0; kb < p.kblocks; ++kb) {
+          for (int kb0 = 0; kb0 < p.kblocks && ok; kb0 += kWords) {
             const uint32_t sa = tmem + kScaleColumn + 32u * buf, sb = sa + 16u;
-            if (kb % kWords == 0) {
-              // (a buffer that is filled again has been used: the warps that fill it waited for its MMAs. The peer's threads
-              // wrote half of it)
-              while (ok && !bar_try(bar_scale(buf), parity_scale)) ok = wait_ok(bar_scale(buf), parity_scale);
-              if (!ok) break;
-              if (lead)
-#pragma unroll
-                for (int i = 0; i < 3; ++i) copy_scales(sa + (i == 0 ? 0 : 12 + 4 * i), scale0 + buf * kScaleBytes + i * 512);
-            }
-            if (kb % kPart == 0 && !(ok = wait_ok(bar_read, parity_acc))) break;
-            if (!(ok = wait_ok(bar_full(s), parity))) break;
+            // (a buffer that is filled again has been used: the warps that fill it waited for its MMAs. The peer's threads
+            // wrote half of it)
+            while (ok && !bar_try(bar_scale(buf), parity_scale)) ok = wait_ok(bar_scale(buf), parity_scale);
+            const bool part_begins = kb0 % kPart == 0;
+            if (!ok || (part_begins && !(ok = wait_ok(bar_read, parity_acc)))) break;
+            if (part_begins) parity_acc ^= 1u;
             fence_after();
-            const uint64_t da = desc0 + s * (kStageBytes >> 4), db = da + (kOperandBytes >> 4);
-            const uint32_t idesc = scaled_desc(kTile, kTile, kb % kWords);
-            const bool part_ends = kb + 1 == p.kblocks || (kb + 1) % kPart == 0;
-            const bool word_ends = kb + 1 == p.kblocks || (kb + 1) % kWords == 0;
-            if (lead) {
+            if (lead)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
-                mma_scaled(tmem, da + 2u * k, db + 2u * k, idesc, sa, sb, k > 0 || kb % kPart > 0);
-              commit_pair(bar_empty(s));
-              if (word_ends) commit_pair(bar_used(buf));
-              if (part_ends) commit_pair(bar_acc);
+              for (int i = 0; i < 3; ++i) copy_scales(sa + (i == 0 ? 0 : 12 + 4 * i), scale0 + buf * kScaleBytes + i * 512);
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+              if (kb0 + j >= p.kblocks || !(ok = wait_ok(ring.full, ring.parity))) break;
+              fence_after();
+              if (lead) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)  // 32 bytes on in K: two units of the address field
+                  mma_scaled(tmem, operand_at(ring.low + 2u * k), operand_at(ring.low + (kOperandBytes >> 4) + 2u * k),
+                             scaled_desc(kTile, kTile, j), sa, sb, j > 0 || k > 0 || !part_begins);
+                commit_pair(ring.empty);
+              }
+              ring.next();
             }
-            if (part_ends) parity_acc ^= 1u;
-            if (word_ends && ++buf == kScaleBuffers) {
+            if (ok && lead) {
+              commit_pair(bar_used(buf));
+              if (kb0 + kWords >= p.kblocks || (kb0 + kWords) % kPart == 0) commit_pair(bar_acc);
+            }
+            if (++buf == kScaleBuffers) {
               buf = 0;
               parity_scale ^= 1u;
-            }
-            if (++s == kStages) {
-              s = 0;
-              parity ^= 1u;
             }
           }
         }
