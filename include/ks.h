@@ -132,6 +132,7 @@ enum { KS_F32 = 0, KS_BF16 = 1, KS_F16 = 2, KS_E4M3 = 3 };
 /* How the scale of a block is stored: fp32, or one byte b that stands for 2^(b - 127) (255: no number). */
 enum { KS_SCALE_F32 = 0, KS_SCALE_E8M0 = 1 };
 #define KS_SCALE_BLOCK 128 /* columns that share a scale */
+#define KS_MAX_EXTENT 2147482624 /* rows or columns of the operators' arrays: 2^31 - 1,024 */
 
 /* What of a row's distribution ks_sample draws from. 16 bytes. */
 typedef struct {
@@ -394,30 +395,32 @@ ks_status ks_quantize_e4m3(ks_ctx* ctx, const void* d_x, int x_type, int64_t row
  *                   does the fp32 sums, scales of scale_type to d_d_scale [m][ceil(n / 128)]; d_d and ldd as d_q and ldq there
  *   d_d_scale       only for KS_E4M3, else NULL
  * The scales' products sa * sb have to be fp32 numbers; d_d may overlap none of the inputs. m == 0 or n == 0 does nothing;
- * k == 0 is the empty sum. Asynchronous on `stream`. m, n, k < 2^31. KS_ERR_UNSUPPORTED where a grid would not hold m. */
+ * k == 0 is the empty sum. The same call gives the same bits. Asynchronous on `stream`; no workspace. m, n, k <= KS_MAX_EXTENT;
+ * KS_ERR_UNSUPPORTED where a grid would not hold them. */
 ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const void* d_a_scale, const uint8_t* d_b, int64_t ldb,
                          const void* d_b_scale, int scale_type, int64_t m, int64_t n, int64_t k, const float* d_bias, int relu,
                          void* d_d, int64_t ldd, int d_type, void* d_d_scale, void* stream);
 
 /* Draws from the softmax of scores, for callers that answer with a distribution rather than with its best candidates (ks_select):
  * candidates to be measured, a policy that explores. A row's scores x_0 .. x_{c-1} get weights w_j = exp((x_j - max) /
- * temperature); a score that is not a number counts as -inf, whose weight is 0, and where the largest score is +inf its holders alone have weight, the same each.
+ * temperature); a score that is not a number counts as -inf, whose weight is 0, and where the largest score is +inf its holders
+ * alone have weight, the same each. A distance from the best score that is no fp32 number counts as infinite.
  * In the order (score descending, index ascending) the first top_k stay; of these the shortest front whose weights sum to at
  * least top_p of theirs (at least one); of these those with w_j >= min_p. With s the sum of what stays, a draw for u in [0, 1) is
  * the first candidate in the order of the indices up to which the weights that stay sum to more than u s.
  * Temperature 0: the best candidate (the first of those that share the score), whatever u.
  *   d_scores       device, score_type KS_F32, KS_BF16 or KS_F16. Without d_seg_offsets row i is [i * ld, i * ld + c), ld >= c; with it
  *                  (P + 1 non-decreasing entries) row i is [d_seg_offsets[i], d_seg_offsets[i + 1]), c their total length (it
- *                  decides how the work is shared out, not what is drawn), and ld is not used. A row has at most 2^31 - 1 scores
+ *                  decides how the work is shared out, not what is drawn), and ld is not used. A row has at most KS_MAX_EXTENT scores
  *   d_params       device, [P], settings of each row, or NULL: *h_params for all rows. Of d_params a temperature that is not
  *                  above 0 counts as 0, top_k < 1 as 0, top_p not below 1 as 1, min_p not above 0 as 0
  *   d_u            device, [P][draws] fp32; below 0 counts as 0, from 1 on as the largest below 1. 1 <= draws <= KS_MAX_K
  *   d_idx          device, [P][draws]: positions in the row; -1 where every weight is 0 (an empty row, all scores -inf)
  *   d_logp         device, [P][draws], or NULL: log(w_j / s) of the candidate drawn; -inf beside -1
- * Weights are held to 2^-52 of the best one's (rows of more than 1,023 scores: to 2^-62 times the power of two above their
- * number); what lies below half of that is never drawn. Draws do not depend on how the work is shared out: the same call gives the same bits. Asynchronous on
- * `stream`; no workspace. KS_ERR_INVALID_ARG for draws out of range, a negative size, or *h_params with a setting that is no number,
- * negative, or top_p outside (0, 1], min_p above 1. */
+ * Weights are held to 2^-51 of the best one's (rows of more than 2,047 scores: to 2^-62 times the power of two above their
+ * number), and their sums are exact; what lies below half of that is never drawn. Draws do not depend on how the work is shared
+ * out: the same call gives the same bits. Asynchronous on `stream`; no workspace. KS_ERR_INVALID_ARG for draws out of range, a
+ * negative size, or *h_params with a setting that is no number, negative, or top_p outside (0, 1], min_p above 1. */
 ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, int64_t c, int64_t ld, const int64_t* d_seg_offsets,
                     const ks_sampling* h_params, const ks_sampling* d_params, const float* d_u, int draws, int32_t* d_idx,
                     float* d_logp, void* stream);

@@ -151,8 +151,9 @@ def _rows(t):
     ld, step = t.stride()
     if not t.is_cuda or (cols > 1 and step != 1):
         raise ValueError("expected a CUDA matrix with contiguous rows")
-    # (torch gives a single row, or one of no columns, any stride)
-    return t.data_ptr(), ld if rows > 1 or ld > cols else cols
+    if cols == 0 or (rows <= 1 and ld < cols):  # (torch gives a single row, or rows without columns, any stride)
+        ld = cols
+    return t.data_ptr(), ld
 
 
 def _flat(t):
@@ -555,7 +556,8 @@ class Context:
                params=None, d_seg_off=None, out_idx=None, out_logp=None):
         """Draws from the softmax of scores ([P, C], or flat with the P + 1 offsets d_seg_off) for the given random
         numbers u [P, draws]. `params`: [P] SAMPLING_DT records on the device (to_device), settings of each row
-        instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each."""
+        instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each; with an
+        out_idx and no out_logp the second is None and not computed."""
         P, draws = u.shape
         if u.dtype != torch.float32 or scores.dtype not in _TYPES:
             raise ValueError("sample: element types")
@@ -572,10 +574,12 @@ class Context:
             raise ValueError("sample: params")
         if out_idx is None:
             out_idx = torch.empty((P, draws), dtype=torch.int32, device=self.device)
-            out_logp = torch.empty((P, draws), dtype=torch.float32, device=self.device)
-        elif out_idx.shape != u.shape or out_idx.dtype != torch.int32 or (
-                out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32)):
-            raise ValueError("sample: out_idx, out_logp")
+            if out_logp is None:
+                out_logp = torch.empty((P, draws), dtype=torch.float32, device=self.device)
+        elif out_idx.shape != u.shape or out_idx.dtype != torch.int32:
+            raise ValueError("sample: out_idx")
+        if out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32):
+            raise ValueError("sample: out_logp")
         one = None if params is not None else ctypes.byref(_Sampling(temperature, top_k, top_p, min_p))
         status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params),
                                 _flat(u), draws, _flat(out_idx), None if out_logp is None else _flat(out_logp),

@@ -225,7 +225,7 @@ ks_status check_pairs(int P, int C, const void* seg_off, const void* seg_idx, in
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 bool aligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
-constexpr int64_t kMaxExtent = INT32_MAX;  // of the arrays of the eight-bit operators
+constexpr int64_t kMaxExtent = KS_MAX_EXTENT;
 
 }  // namespace
 
@@ -382,7 +382,7 @@ ks_status ks_model_describe(const ks_model* model, char* buf, int len) {
   } else if (model->kind == 1 && model->mlp.h_ridge) {
     std::snprintf(buf, len, "select_ridge_kernel");
   } else if (model->kind == 1 && ks::is_e4m3_mlp(model->mlp)) {
-    std::snprintf(buf, len, "matmul_pair_kernel layers=%d", model->mlp.n_layers);
+    std::snprintf(buf, len, "matmul_scaled_kernel layers=%d", model->mlp.n_layers);
   } else if (model->kind == 1) {
     std::snprintf(buf, len, "mlp_wide_kernel layers=%d", model->mlp.n_layers);
   } else {
@@ -907,8 +907,10 @@ ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, in
       return KS_ERR_INVALID_ARG;
   }
   if (P == 0) return KS_OK;
-  if (!d_u || !d_idx || (!d_scores && (d_seg_offsets || c > 0))) return KS_ERR_INVALID_ARG;
-  if (!aligned(d_scores, score_type == KS_F32 ? 4 : 2) || !aligned(d_params, 4) || !aligned(d_seg_offsets, 8)) return KS_ERR_INVALID_ARG;
+  if (!d_u || !d_idx || (!d_scores && c > 0)) return KS_ERR_INVALID_ARG;
+  if (!aligned(d_scores, score_type == KS_F32 ? 4 : 2) || !aligned(d_params, 4) || !aligned(d_seg_offsets, 8) ||
+      !aligned(d_u, 4) || !aligned(d_idx, 4) || !aligned(d_logp, 4))
+    return KS_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);
   const ks::SampleArgs a{d_scores, ld, d_seg_offsets, P, c, d_params ? ks_sampling{} : *h_params, d_params, d_u, draws, d_idx, d_logp};
   cudaError_t e = ks::launch_sample(a, score_type, static_cast<cudaStream_t>(stream), &ctx->launches);

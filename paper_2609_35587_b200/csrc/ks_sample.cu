@@ -17,9 +17,13 @@
 // k-th score from below, so that little more than k candidates are listed, sorted, cut, and drawn from in the list.
 //
 // A row of a call with few rows belongs to a cluster of up to 16 CTAs that keep its scores in shared memory, each thread its
-// own; the CTAs' results meet there too. Where there are rows for the whole machine a CTA takes a row by itself and reads it
-// again in every phase, mostly from L2: four smaller CTAs an SM hide each other's barriers, of which a cluster has more and
-// longer ones (1,024 x 60,000 scores: 947 us by clusters of 4).
+// own; the CTAs' results meet there too. Where there are rows for the whole machine a CTA takes a row by itself: short ones are
+// kept, by four CTAs an SM, long ones read again in every phase by two CTAs an SM, which is what stays in L2 (1,024 x 60,000
+// scores with top-k 50: 298 us by four CTAs, 217 by two; with top-p 0.95 as it was then 416 and 410, by clusters of four 947).
+//
+// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 365 us where reading them takes 38: three passes, of
+// which the one with the weights (20 operations in 64 bits and the sums) takes half; the issue slots are 67 % busy, the fp64
+// pipe 13 %. Single rows are bound by the clusters' meetings: 60,000 scores with top-k and top-p 15 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -318,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, d));
   }
   // the maxima of the parts, and the one that as many of them reach as the CTA's share of a short front has candidates
-  const int share = (set.top_k + ctas - 1) / ctas;
+  const int share = (min(set.top_k, kShort) + ctas - 1) / ctas;
   const bool short_front = !greedy && set.top_k > 0 && set.top_k <= kShort && share <= kShortParts;
   if (short_front) {
     constexpr int kEach = kThreads / kParts;
@@ -383,7 +387,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   r.steps = greedy ? 0.0 : kTable * 1.4426950408889634074 / static_cast<double>(set.temperature);
   r.one = ldexp(1.0, min(51, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
   r.least = set.min_p > 0.0f ? fmin(static_cast<double>(set.min_p), 1.0) * r.one : 0.0;
-  r.reach = greedy ? 0.0f : (kReach + 1.0f) * set.temperature;
+  // (finite, so that it leaves out -inf at any temperature)
+  r.reach = greedy ? 0.0f : fminf((kReach + 1.0f) * set.temperature, 3.402823466e38f);
   // bins over what the scores reach, but no further than weights do
   const float span = fminf(r.best - low, kReach * set.temperature);
   r.bins = span > 0.0f ? static_cast<float>(kBins - 1) / span : 0.0f;

@@ -202,3 +202,46 @@ def test_one_pass_quantised_layer_scored_and_drawn(ctx):
     u = numbers(rows // per, 8, 14)
     idx, logp = ctx.sample(scores.view(-1), u, temperature=0.3, top_k=20, d_seg_off=off)
     check(scores.view(-1), u, idx, logp, rows=off.cpu().numpy(), t=0.3, top_k=20)
+
+
+def test_rows_without_a_score(ctx):
+    """No columns, segments that are all empty, no rows."""
+    u = numbers(3, 2, 1)
+    idx, logp = ctx.sample(torch.empty(3, 0, device=DEV), u, top_p=0.5)
+    assert idx.tolist() == [[-1, -1]] * 3 and bool((logp == -np.inf).all())
+    idx, logp = ctx.sample(torch.empty(0, device=DEV), u, top_k=4, d_seg_off=torch.zeros(4, dtype=torch.int64, device=DEV))
+    assert idx.tolist() == [[-1, -1]] * 3 and bool((logp == -np.inf).all())
+    idx, _ = ctx.sample(torch.empty(0, 5, device=DEV), torch.empty(0, 2, device=DEV))
+    assert idx.shape == (0, 2)
+
+
+@pytest.mark.parametrize("p,c", [(1, 3000), (2, 60000), (300, 3000), (300, 20000), (1, 1000003)])
+@pytest.mark.parametrize("s", [dict(top_p=0.6), dict(top_k=700, top_p=0.8), dict(top_k=300), dict(top_k=2000, min_p=0.01)], ids=str)
+@pytest.mark.parametrize("values", ["equal", "two", "steps", "far", "huge"])
+def test_scores_that_crowd(ctx, p, c, s, values):
+    """Scores of which far more than a sorted list holds share a bin or a value, or lie where fp32 has no more room."""
+    g = torch.Generator().manual_seed(c)
+    x = {"equal": torch.full((p, c), 1.5), "two": torch.randint(0, 2, (p, c), generator=g).float(),
+         "steps": torch.randint(0, 7, (p, c), generator=g).float() * 0.25,
+         "far": torch.where(torch.rand(p, c, generator=g) < 0.001, torch.tensor(0.0), torch.tensor(-30.0)),
+         "huge": torch.randn(p, c, generator=g) * 1e37}[values]
+    x = x.to(DEV)
+    u = numbers(p, 3, p)
+    idx, logp = draw(ctx, x, u, **s)
+    rows = range(p) if p < 10 else range(0, p, 60)
+    for r in rows:
+        lowbit.check_draws(lowbit.as_float64(x[r]), u[r].cpu().numpy(), idx[r].cpu().numpy(), logp[r].cpu().numpy(), **s)
+
+
+@pytest.mark.parametrize("t", [1e-38, 1e-3, 1e30, float("inf")])
+def test_temperatures_from_device_memory(ctx, t):
+    """Very small ones leave the best score, very large ones make all alike; settings of device memory are not refused."""
+    x = torch.randn(3, 500, generator=torch.Generator().manual_seed(3))
+    x[1, 7] = x[1, 400] = 9.0
+    x[2, 3] = -np.inf
+    x = x.to(DEV)
+    rec = np.zeros(3, ks.SAMPLING_DT)
+    rec["temperature"], rec["top_p"] = t, 0.9
+    u = numbers(3, 4, 2)
+    idx, logp = ctx.sample(x, u, params=ks.to_device(rec, DEV))
+    check(x, u, idx, logp, t=t, top_p=0.9)

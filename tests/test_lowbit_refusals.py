@@ -9,6 +9,7 @@ from paper_2609_35587_b200 import binding as ks
 
 CTX = ctypes.create_string_buffer(4096)
 P = 1 << 20  # an address that is never used
+OVER = (1 << 31) - 1023  # rows or columns, one too many
 
 
 def call(fn, *args):
@@ -27,7 +28,8 @@ def quantize(**kw):
 @pytest.mark.parametrize("bad", [
     dict(x=None), dict(q=None), dict(scale=None), dict(x_type=3), dict(x_type=-1), dict(rows=-1), dict(cols=-1), dict(ldx=199),
     dict(ldq=199), dict(ldq=200), dict(q=P + 8), dict(x=P + 2), dict(block_rows=64), dict(block_rows=0), dict(scale_type=2),
-    dict(scale=P + 2, scale_type=ks.KS_SCALE_F32), dict(rows=1 << 31), dict(cols=1 << 31, ldx=1 << 31, ldq=1 << 31)])
+    dict(scale=P + 2, scale_type=ks.KS_SCALE_F32), dict(rows=1 << 31), dict(cols=1 << 31, ldx=1 << 31, ldq=1 << 31),
+    dict(rows=OVER), dict(cols=OVER, ldx=1 << 31, ldq=1 << 31)])
 def test_quantize(bad):
     assert quantize(**bad) == ks.KS_ERR_INVALID_ARG
 
@@ -54,7 +56,8 @@ def matmul(**kw):
     dict(a=None), dict(b=None), dict(sa=None), dict(sb=None), dict(d=None), dict(lda=199), dict(lda=200), dict(ldb=192), dict(ldb=216),
     dict(a=P + 8), dict(b=P + 4), dict(sa=P + 1), dict(sb=P + 2), dict(bias=P + 2), dict(d=P + 2), dict(ldd=7), dict(m=-1), dict(n=-1),
     dict(k=-1), dict(m=1 << 31), dict(d_type=4), dict(d_type=-1), dict(scale_type=7), dict(sd=P), dict(d_type=ks.KS_E4M3),
-    dict(d_type=ks.KS_E4M3, sd=P, ldd=8), dict(d_type=ks.KS_E4M3, sd=P, ldd=16, d=P + 1), dict(d_type=ks.KS_E4M3, sd=P + 2, ldd=16)])
+    dict(d_type=ks.KS_E4M3, sd=P, ldd=8), dict(d_type=ks.KS_E4M3, sd=P, ldd=16, d=P + 1), dict(d_type=ks.KS_E4M3, sd=P + 2, ldd=16),
+    dict(m=OVER), dict(n=OVER, ldd=1 << 31), dict(k=OVER, lda=1 << 31, ldb=1 << 31)])
 def test_matmul(bad):
     assert matmul(**bad) == ks.KS_ERR_INVALID_ARG
 
@@ -74,7 +77,7 @@ def sample(**kw):
     dict(scores=None), dict(u=None), dict(idx=None), dict(P=-1), dict(c=-1), dict(ld=9), dict(c=1 << 31, ld=1 << 31), dict(seg=P, c=-1), dict(draws=0), dict(draws=33), dict(score_type=3),
     dict(score_type=-1), dict(scores=P + 2), dict(params=P + 2), dict(seg=P + 4), dict(none=True), dict(t=-1.0), dict(t=float("nan")),
     dict(t=float("inf")), dict(top_k=-1), dict(top_p=0.0), dict(top_p=1.5), dict(top_p=float("nan")), dict(min_p=-0.1), dict(min_p=1.1),
-    dict(min_p=float("nan"))])
+    dict(min_p=float("nan")), dict(c=OVER, ld=1 << 31), dict(u=P + 2), dict(idx=P + 1), dict(logp=P + 2)])
 def test_sample(bad):
     assert sample(**bad) == ks.KS_ERR_INVALID_ARG
 
