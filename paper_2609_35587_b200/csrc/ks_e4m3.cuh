@@ -19,11 +19,6 @@ template <> __device__ __forceinline__ float to_float(float v) { return v; }
 template <> __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 template <> __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
 
-template <typename T> __device__ __forceinline__ T from_float(float v);
-template <> __device__ __forceinline__ float from_float(float v) { return v; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
-
 // What an element adds to its block's maximum: values that are not finite do not count.
 __device__ __forceinline__ float finite_abs(float v) {
   const float a = fabsf(v);

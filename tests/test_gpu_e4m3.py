@@ -165,6 +165,17 @@ def test_matmul_quantised_result(ctx, m, n, k, scale):
     assert bool((wide[m:] == 0x55).all()) and bool((wide[:, n:] == 0x55).all())
 
 
+@pytest.mark.parametrize("m", [3, 300])
+@pytest.mark.parametrize("scale", [torch.float32, torch.float8_e8m0fnu])
+def test_matmul_empty_sum_of_many_rows(ctx, m, scale):
+    a, b = torch.empty(m, 0, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(130, 0, dtype=torch.float8_e4m3fn, device=DEV)
+    bias = torch.arange(130.0, device=DEV) - 60
+    sa, sb = (torch.empty(r, 0, device=DEV).to(scale) for r in (m, 2))
+    got = ctx.matmul_e4m3(a, sa, b, sb, bias=bias, relu=True, out_dtype=torch.float32)
+    assert torch.equal(got, bias.clamp(min=0).expand(m, 130))
+    assert not bool(ctx.matmul_e4m3(a, sa, b, sb).any())
+
+
 def test_matmul_empty_sum(ctx):
     a = torch.empty(3, 16, device=DEV).to(torch.float8_e4m3fn)[:, :0]
     s = torch.empty(3, 0, device=DEV)
@@ -224,6 +235,49 @@ def test_matmul_same_bits_in_streams_and_graphs(ctx, m, n, k):
         graph.replay()
         q2, s2 = ctx.quantize_e4m3(x)
         assert torch.equal(out, ctx.matmul_e4m3(q2, s2, b, sb))
+
+
+def test_matmul_long_sums(ctx):
+    """Many blocks of K: several parts of an accumulator, several chunks of scales, ends inside both."""
+    for m, n, k in ((130, 130, 4096 + 128 * 3 + 5), (20, 70, 20000), (257, 100, 12345)):
+        for scale in ("e8m0", "f32"):
+            (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, n, k, scale, 2)
+            want, mag = lowbit.matmul(av, sav, bv, sbv)
+            got = ctx.matmul_e4m3(a, sa, b, sb, out_dtype=torch.float32)
+            assert (np.abs(lowbit.as_float64(got) - want) <= off_by(k, mag, want, torch.float32)).all()
+
+
+@pytest.mark.parametrize("m", [30, 300])
+def test_matmul_scale_that_is_no_number(ctx, m):
+    """The byte 255 spoils its row's sums."""
+    (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, 140, 300, "e8m0", 4)
+    sa.view(torch.uint8)[5, 1] = 255
+    want, mag = lowbit.matmul(av, sav, bv, sbv)
+    got = lowbit.as_float64(ctx.matmul_e4m3(a, sa, b, sb, out_dtype=torch.float32))
+    assert np.isnan(got[5]).all()
+    rest = np.arange(m) != 5
+    assert (np.abs(got - want)[rest] <= off_by(300, mag, want, torch.float32)[rest]).all()
+
+
+def test_two_graphs_and_an_eager_call(ctx):
+    """Two captured products replayed in turn with a call in between: they share nothing."""
+    sets = []
+    for seed, m in ((1, 20), (2, 300)):
+        (a, sa, _, _), (b, sb, _, _) = operands(m, 200, 300, "e8m0", seed)
+        out = ctx.matmul_e4m3(a, sa, b, sb)
+        want = out.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.matmul_e4m3(a, sa, b, sb, out=out)
+        sets.append((graph, out, want, (a, sa, b, sb)))
+    for _ in range(3):
+        for graph, out, _, _ in sets:
+            out.zero_()
+            graph.replay()
+        eager = ctx.matmul_e4m3(*sets[0][3])
+        for _, out, want, _ in sets:
+            assert torch.equal(out, want)
+        assert torch.equal(eager, sets[0][2])
 
 
 def test_binding_refuses(ctx):

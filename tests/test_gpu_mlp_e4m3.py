@@ -81,7 +81,7 @@ def by_layers(ctx, x, mlp, onehot):
 def test_scores(ctx, onehot, hidden, P, C):
     mlp = make(onehot, hidden, len(hidden))
     model = ctx.model_create_mlp_e4m3(mlp)
-    assert "matmul_pair_kernel" in model.describe()
+    assert "matmul_scaled_kernel" in model.describe()
     _, _, _, x = features(ctx, P, C)
     x[0, 40], x[0, 41] = float("nan"), float("inf")
     got = lowbit.as_float64(ctx.score(x, model))
