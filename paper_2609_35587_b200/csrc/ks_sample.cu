@@ -50,6 +50,7 @@ constexpr int kMaxCtas = 16;       // of a cluster
 constexpr int kParts = 128;        // of a CTA's scores, whose maxima bound a short front
 constexpr int kShort = 512, kShortParts = 112;  // the longest front that is drawn from a list, and its share of a CTA's parts
 constexpr int kHeldLoads = 8;      // 16-byte loads that a thread keeps at most
+constexpr int kShortRow = 256;     // scores of a row that a warp takes
 constexpr int kEntries = 1024;     // sums over stretches of a row that a CTA keeps
 constexpr float kReach = 36.05f;   // (best - x) / t behind which every weight rounds to 0 (51 bits)
 constexpr int kTable = 256;        // powers of two within one octave
@@ -68,7 +69,8 @@ struct Row {
 // Weight of a score within reach in units of 2^-s, before it is rounded: 2^(n / 256) from a table of 256 (times 2^s) and the
 // exponent, times the exponential of what is left, at most ln 2 / 512, by its series (P. T. P. Tang's table-driven method, ACM
 // TOMS 15, 1989). The first term that is left out is below 2^-54. The best score's weight is exact, also where it is infinite.
-__device__ __forceinline__ double scaled_weight(const Row& r, const double* table, float x) {
+template <typename Table>
+__device__ __forceinline__ double scaled_weight(const Row& r, const Table& table, float x) {
   constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: adding it rounds to a whole number in the low word
   constexpr double kL = 0.69314718055994530942 / kTable;
   const double z = (static_cast<double>(x) - r.best_wide) * r.steps, m = z + kRound;
@@ -82,6 +84,19 @@ __device__ __forceinline__ double scaled_weight(const Row& r, const double* tabl
   const double v = __hiloint2double(__double2hiint(w) + ((n >> 8) << 20), __double2loint(w));
   return x == r.best ? r.one : v;
 }
+__device__ __forceinline__ Row row_of(const ks_sampling& set, bool greedy, float best, int len) {
+  Row r;
+  r.best = best;
+  r.best_wide = static_cast<double>(best);
+  r.steps = greedy ? 0.0 : kTable * 1.4426950408889634074 / static_cast<double>(set.temperature);
+  r.one = ldexp(1.0, min(51, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
+  r.least = set.min_p > 0.0f ? fmin(static_cast<double>(set.min_p), 1.0) * r.one : 0.0;
+  // (finite, so that it leaves out -inf at any temperature)
+  r.reach = greedy ? 0.0f : fminf((kReach + 1.0f) * set.temperature, 3.402823466e38f);
+  r.bins = 0.0f;
+  return r;
+}
+__device__ __forceinline__ double power(int i, double one) { return exp2(static_cast<double>(i) / kTable) * one; }
 // rounded; w <= 2^51, so that the sum's low bits are the whole number
 __device__ __forceinline__ Wide whole(double w) {
   return static_cast<Wide>(__double_as_longlong(w + 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
@@ -216,8 +231,153 @@ __device__ __noinline__ uint4 fetch_edge(const T* base, uint32_t at, uint32_t sh
   return make_uint4(u[0], u[1], u[2], u[3]);
 }
 
+// ---- short rows ----
+
+// Keys of a warp, E neighbours a lane, descending.
+template <int E>
+__device__ __forceinline__ void sort_keys(Wide (&x)[E], int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32 * E; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2)
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        const bool down = ((lane * E + q) & k) == 0;
+        if (j >= E) {
+          const Wide y = __shfl_xor_sync(0xFFFFFFFFu, x[q], j / E);
+          if ((((lane * E + q) & j) == 0) == down == (y > x[q])) x[q] = y;
+        } else if ((q & j) == 0) {
+          const Wide u = x[q], v = x[q | j];
+          if ((u < v) == down) {
+            x[q] = v;
+            x[q | j] = u;
+          }
+        }
+      }
+}
+
+struct Powers {
+  double one;
+  __device__ __forceinline__ double operator[](int i) const { return power(i, one); }
+};
+
+// A row of up to 32 * E scores by one warp, without a barrier, E neighbours a lane: the best one, the cuts from a sorted copy where
+// there are cuts, the sums up to each score, which are searched. The same weights and sums as sample_kernel's, so the same draws.
+template <typename T, int E>
+__device__ __noinline__ void short_row(const SampleArgs& a, int64_t p, const T* row, int len, const ks_sampling& set, Wide* upto) {
+  const int lane = threadIdx.x % 32, first = lane * E;
+  const float none = __int_as_float(0xFF800000);
+  auto place = [](int i) KS_INLINE { return i + i / E; };  // (no two lanes' in one bank)
+  float y[E];
+  Wide best = 0;
+#pragma unroll
+  for (int q = 0; q < E; ++q) y[q] = first + q < len ? normal(to_float(row[first + q])) : none;
+  auto key = [&](int q) KS_INLINE -> Wide { return y[q] > none ? make_key(y[q], first + q) : 0; };
+#pragma unroll
+  for (int q = 0; q < E; ++q) best = max(best, key(q));
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) best = max(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
+  if (best == 0) {  // nothing has weight
+    for (int q = lane; q < a.draws; q += 32) {
+      a.idx[p * a.draws + q] = -1;
+      if (a.logp) a.logp[p * a.draws + q] = none;
+    }
+    return;
+  }
+  const bool greedy = !(set.temperature > 0.0f);
+  const Row r = row_of(set, greedy, key_score(best), len);
+  const Powers powers{r.one};
+  Wide cut = greedy ? best : 0;  // what stays has this key or a larger one
+  const bool some = set.top_k > 0 && set.top_k < len, front = set.top_p < 1.0f;
+  if (!greedy && (some || front)) {
+    Wide x[E];
+#pragma unroll
+    for (int q = 0; q < E; ++q) x[q] = key(q);
+    sort_keys<E>(x, lane);
+    if (some) {
+      Wide mine = 0;
+#pragma unroll
+      for (int q = 0; q < E; ++q)
+        if (q == (set.top_k - 1) % E) mine = x[q];
+      cut = __shfl_sync(0xFFFFFFFFu, mine, (set.top_k - 1) / E);
+    }
+    if (front) {
+      Wide w[E], sum = 0;
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        const float v = key_score(x[q]);
+        w[q] = x[q] < cut || r.best - v > r.reach ? 0 : whole(scaled_weight(r, powers, v));
+        sum += w[q];
+      }
+      const Wide end = warp_scan(sum, lane), total = __shfl_sync(0xFFFFFFFFu, end, 31);
+      const Wide target = max(1ull, static_cast<Wide>(ceil(fmax(static_cast<double>(set.top_p), 0.0) * static_cast<double>(total))));
+      Wide before = end - sum, last = 0;
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        if (before < target && before + w[q] >= target) last = x[q];
+        before += w[q];
+      }
+      const unsigned who = __ballot_sync(0xFFFFFFFFu, last > 0);
+      if (who) cut = __shfl_sync(0xFFFFFFFFu, last, __ffs(who) - 1);
+    }
+  }
+  Wide w[E], sum = 0;
+#pragma unroll
+  for (int q = 0; q < E; ++q) {
+    const double exact = scaled_weight(r, powers, y[q]);
+    const bool stays = key(q) >= cut && !(r.best - y[q] > r.reach) && (greedy || exact >= r.least);
+    w[q] = stays ? greedy ? 1 : whole(exact) : 0;
+    sum += w[q];
+  }
+  Wide end = warp_scan(sum, lane);
+  const Wide all = __shfl_sync(0xFFFFFFFFu, end, 31);
+  end -= sum;
+#pragma unroll
+  for (int q = 0; q < E; ++q) upto[place(first + q)] = end += w[q];
+  __syncwarp();
+  for (int q = lane; q < a.draws; q += 32) {
+    const float u = a.u[p * a.draws + q];
+    Wide goal = static_cast<Wide>(static_cast<double>(u > 0.0f ? u : 0.0f) * static_cast<double>(all));
+    if (u >= 1.0f || goal >= all) goal = all - 1;
+    int lo = 0;  // the first whose end is behind the goal
+#pragma unroll
+    for (int step = 16 * E; step > 0; step /= 2)
+      if (upto[place(lo + step - 1)] <= goal) lo += step;
+    a.idx[p * a.draws + q] = lo;
+    if (a.logp) {
+      const float v = normal(to_float(row[lo]));
+      const double d = v == r.best ? 0.0 : (static_cast<double>(v) - r.best_wide) / static_cast<double>(set.temperature);
+      a.logp[p * a.draws + q] = static_cast<float>(d - log(static_cast<double>(all) / (greedy ? 1.0 : r.one)));
+    }
+  }
+}
+
+constexpr int kShortWarps = 4;
+constexpr int kShortPlaces = kShortRow + 32;
+// Rows of up to kShortRow scores by a warp each; others are left.
+template <typename T>
+__global__ void __launch_bounds__(32 * kShortWarps) short_rows_kernel(const __grid_constant__ SampleArgs a) {
+  static_assert(kShortRow == 32 * 8, "the longest row has eight scores a lane");
+  __shared__ Wide s[kShortWarps][kShortPlaces];
+  next_may_start();
+  wait_for_last();
+  const int64_t p = static_cast<int64_t>(blockIdx.x) * kShortWarps + threadIdx.x / 32;
+  if (p >= a.p) return;
+  const int64_t begin = a.seg_off ? a.seg_off[p] : p * a.ld;
+  const int64_t scores = a.seg_off ? a.seg_off[p + 1] - begin : a.c;
+  if (scores > kShortRow) return;
+  const int len = static_cast<int>(scores);
+  const T* row = static_cast<const T*>(a.scores) + begin;
+  const ks_sampling set = a.params ? a.params[p] : a.all;
+  Wide* mine = s[threadIdx.x / 32];
+  if (len <= 32) short_row<T, 1>(a, p, row, len, set, mine);
+  else if (len <= 64) short_row<T, 2>(a, p, row, len, set, mine);
+  else if (len <= 128) short_row<T, 4>(a, p, row, len, set, mine);
+  else short_row<T, 8>(a, p, row, len, set, mine);
+}
+
 template <typename T, int kThreads>
-__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const __grid_constant__ SampleArgs a, int ctas, int held_loads) {
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const __grid_constant__ SampleArgs a, int ctas, int held_loads, int done) {
   constexpr int kWarps = kThreads / 32;
   __shared__ Shared<kWarps> s;
   extern __shared__ uint4 s_held[];  // [held_loads][threads]
@@ -228,10 +388,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   const int64_t p = blockIdx.x / ctas;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int64_t begin = a.seg_off ? a.seg_off[p] : p * a.ld;
-  const int len = static_cast<int>(a.seg_off ? a.seg_off[p + 1] - begin : a.c);
+  const int len = static_cast<int>(a.seg_off ? max(a.seg_off[p + 1] - begin, static_cast<int64_t>(0)) : a.c);
   const T* row = static_cast<const T*>(a.scores) + begin;
   const ks_sampling set = a.params ? a.params[p] : a.all;
   const float none = __int_as_float(0xFF800000);
+  if (len <= done) return;  // (a short row, drawn from by short_rows_kernel)
 
   // This CTA's stretch of the row, in places that are counted from the last 16-byte boundary at or before its first score. It
   // is kept in shared memory where it fits, one tile, else read again in every phase, in tiles that are few enough for the
@@ -381,18 +542,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     return;
   }
 
-  Row r;
-  r.best = key_score(best);
-  r.best_wide = static_cast<double>(r.best);
-  r.steps = greedy ? 0.0 : kTable * 1.4426950408889634074 / static_cast<double>(set.temperature);
-  r.one = ldexp(1.0, min(51, __clzll(static_cast<long long>(len)) - 2));  // sums of all weights fit 63 bits
-  r.least = set.min_p > 0.0f ? fmin(static_cast<double>(set.min_p), 1.0) * r.one : 0.0;
-  // (finite, so that it leaves out -inf at any temperature)
-  r.reach = greedy ? 0.0f : fminf((kReach + 1.0f) * set.temperature, 3.402823466e38f);
+  Row r = row_of(set, greedy, key_score(best), len);
   // bins over what the scores reach, but no further than weights do
   const float span = fminf(r.best - low, kReach * set.temperature);
   r.bins = span > 0.0f ? static_cast<float>(kBins - 1) / span : 0.0f;
-  if (threadIdx.x < kTable) s.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / kTable) * r.one;
+  if (threadIdx.x < kTable) s.table[threadIdx.x] = power(threadIdx.x, r.one);
   __syncthreads();
   // ---- a short front ----
   if (short_front) {
@@ -932,28 +1086,41 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 }
 
 template <typename T, int kThreads>
-cudaError_t launch_as(const SampleArgs& a, int ctas, int held_loads, cudaStream_t stream) {
+cudaError_t launch_as(const SampleArgs& a, int ctas, int held_loads, int done, cudaStream_t stream) {
   const void* kernel = reinterpret_cast<const void*>(&sample_kernel<T, kThreads>);
   cudaError_t e = ensure_dynamic_smem(kernel, kHeldLoads * kThreads * 16);
   if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return e;
   return launch_following(&sample_kernel<T, kThreads>, dim3(static_cast<unsigned>(a.p * ctas)), kThreads,
-                          static_cast<size_t>(held_loads) * kThreads * 16, ctas, stream, a, ctas, held_loads);
+                          static_cast<size_t>(held_loads) * kThreads * 16, ctas, stream, a, ctas, held_loads, done);
 }
 
 constexpr int kSmall = 256, kLarge = 512;  // threads of a CTA
 constexpr int64_t kManyRows = 296;
 
 template <typename T>
-cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
+cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream, int64_t* launches) {
   constexpr int64_t kV = 16 / sizeof(T);
   const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
+  // Short rows by a warp each: all of a call, or those of many segments or of segments that are short on the average, in a launch of
+  // their own (4,096 rows of 32 scores with top-k: 98 us by CTAs, 6.5 by warps; of 256 scores 98 and 26. Warps of the other
+  // kernel's CTAs instead of a launch: no gain, its code grows).
+  const bool all_short = a.c <= kShortRow, some_short = a.seg_off && (a.p >= kManyRows || len <= kShortRow);
+  if (all_short || some_short) {
+    if (a.p > INT32_MAX) return cudaErrorInvalidConfiguration;
+    const cudaError_t e = launch_following(&short_rows_kernel<T>, dim3(static_cast<unsigned>((a.p + kShortWarps - 1) / kShortWarps)),
+                                           32 * kShortWarps, 0, 0, stream, a);
+    ++*launches;
+    if (e != cudaSuccess || all_short) return e;
+  }
+  const int done = some_short ? kShortRow : -1;
+  ++*launches;
   if (a.p >= kManyRows) {
     // rows that four CTAs an SM keep (28 KB each; segments are of all lengths), else what is in work at a time stays in L2
     constexpr int64_t kKept = 7;
     if (len <= kKept * kSmall * kV)
-      return launch_as<T, kSmall>(a, 1, static_cast<int>(a.seg_off ? kKept : std::min(kKept, (len + 64 * kV) / (kSmall * kV) + 1)), stream);
-    return launch_as<T, kLarge>(a, 1, 0, stream);
+      return launch_as<T, kSmall>(a, 1, static_cast<int>(a.seg_off ? kKept : std::min(kKept, (len + 64 * kV) / (kSmall * kV) + 1)), done, stream);
+    return launch_as<T, kLarge>(a, 1, 0, done, stream);
   }
   int ctas = 1;
   while (ctas < kMaxCtas && kLarge * kV * kHeldLoads * ctas < len) ctas *= 2;
@@ -962,17 +1129,16 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream) {
   if (a.p * ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
   const int64_t each = (a.seg_off ? 2 * len : len + ctas - 1) / ctas + 64 * kV;
   const int64_t loads = std::min<int64_t>(kHeldLoads, (each + kLarge * kV - 1) / (kLarge * kV));
-  return launch_as<T, kLarge>(a, ctas, static_cast<int>(loads), stream);
+  return launch_as<T, kLarge>(a, ctas, static_cast<int>(loads), done, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_sample(const SampleArgs& a, int score_type, cudaStream_t stream, int64_t* launches) {
-  ++*launches;
   switch (score_type) {
-    case KS_F32: return launch_type<float>(a, stream);
-    case KS_BF16: return launch_type<__nv_bfloat16>(a, stream);
-    default: return launch_type<__half>(a, stream);
+    case KS_F32: return launch_type<float>(a, stream, launches);
+    case KS_BF16: return launch_type<__nv_bfloat16>(a, stream, launches);
+    default: return launch_type<__half>(a, stream, launches);
   }
 }
 

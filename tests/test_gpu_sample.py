@@ -245,3 +245,28 @@ def test_temperatures_from_device_memory(ctx, t):
     u = numbers(3, 4, 2)
     idx, logp = ctx.sample(x, u, params=ks.to_device(rec, DEV))
     check(x, u, idx, logp, t=t, top_p=0.9)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("c", [1, 2, 32, 33, 63, 64, 65, 128, 129, 255, 256, 257, 300])
+@pytest.mark.parametrize("s", [dict(), dict(top_p=0.7, min_p=0.05), dict(top_k=33, top_p=0.9), dict(t=0.0), dict(min_p=1.0)], ids=str)
+def test_short_rows(ctx, c, dtype, s):
+    """The same draws from few rows, from many, and from segments among longer ones."""
+    g = torch.Generator().manual_seed(c)
+    p, few = 330, 5
+    x = (torch.randn(p, c, generator=g) * 2).to(dtype)
+    x[1, c // 2], x[2, 0], x[3, c - 1] = float("nan"), float("inf"), -float("inf")
+    x[4] = -float("inf")
+    x[0] = x[0, 0]
+    x = x.to(DEV)
+    u = numbers(p, 33 if c == 64 else 3, c)[:, :32].contiguous()
+    idx, logp = draw(ctx, x, u, **s)
+    check(x[:few], u[:few], idx[:few], logp[:few], **s)
+    check(x[-few:], u[-few:], idx[-few:], logp[-few:], **s)
+    again = draw(ctx, x[:few].contiguous(), u[:few].contiguous(), **s)
+    assert torch.equal(again[0], idx[:few]) and torch.equal(again[1], logp[:few])
+    long = torch.randn(3000, generator=g).to(dtype).to(DEV)
+    flat = torch.cat([torch.cat([x[r], long]) for r in range(few)])
+    lens = torch.tensor([0] + [c, 3000] * few, dtype=torch.int64)
+    seg = draw(ctx, flat, u[:few].repeat_interleave(2, 0).contiguous(), seg_off=lens.cumsum(0).to(DEV), **s)
+    assert torch.equal(seg[0][::2], idx[:few]) and torch.equal(seg[1][::2], logp[:few])
