@@ -164,26 +164,103 @@ __device__ __forceinline__ void meet(int ctas) {
   else cluster_sync();
 }
 
-// The block's list of n <= kList keys, descending.
-template <int kThreads>
-__device__ __forceinline__ void sort_list(Wide* list, int n) {
-  int size = 64;
-  while (size < n) size *= 2;
-  for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = 0;
-  __syncthreads();
-  for (int k = 2; k <= size; k *= 2)
-    for (int j = k / 2; j > 0; j /= 2) {
-      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
-        const int a = 2 * i - (i & (j - 1)), b = a + j;
-        const Wide x = list[a], y = list[b];
-        if ((x < y) == ((a & k) == 0)) {
-          list[a] = y;
-          list[b] = x;
+// Bitonic sorts, descending. Of a warp's keys, E neighbours a lane:
+template <int E, typename Key>
+__device__ __forceinline__ void sort_warp(Key (&x)[E], int lane) {
+#pragma unroll
+  for (int k = 2; k <= 32 * E; k *= 2)
+#pragma unroll
+    for (int j = k / 2; j > 0; j /= 2)
+#pragma unroll
+      for (int q = 0; q < E; ++q) {
+        const int at = lane * E + q;
+        const bool down = (at & k) == 0;
+        if (j >= E) {
+          const Key y = __shfl_xor_sync(0xFFFFFFFFu, x[q], j / E);
+          if (((at & j) == 0) == down == (y > x[q])) x[q] = y;
+        } else if ((q & j) == 0) {
+          const Key u = x[q], v = x[q | j];
+          if ((u < v) == down) {
+            x[q] = v;
+            x[q | j] = u;
+          }
         }
       }
-      if (j > 32 || j == 1) __syncthreads();  // (from 32 down a warp's pairs are its own)
-      else __syncwarp();
+}
+template <int E>
+__device__ __forceinline__ void sort_short(Wide* list, int n) {
+  Wide x[E];
+#pragma unroll
+  for (int q = 0; q < E; ++q) x[q] = static_cast<int>(threadIdx.x) * E + q < n ? list[threadIdx.x * E + q] : 0;
+  sort_warp<E>(x, threadIdx.x);
+#pragma unroll
+  for (int q = 0; q < E; ++q) list[threadIdx.x * E + q] = x[q];
+}
+// Of a block's `size` keys (a power of two) by the warps that have some, partners in other warps through `list`.
+template <int E>
+__device__ __forceinline__ void sort_long(Wide* list, int n, int size) {
+  Wide x[E];
+  const int first = threadIdx.x * E;
+  const bool mine = first < size;
+#pragma unroll
+  for (int q = 0; q < E; ++q) x[q] = first + q < n ? list[first + q] : 0;
+#pragma unroll 1
+  for (int k = 2; k <= size; k *= 2) {
+#pragma unroll 1
+    for (int j = k / 2; j >= E; j /= 2) {
+      const bool far = j >= 32 * E;
+      if (far) {
+        __syncthreads();
+        if (mine)
+#pragma unroll
+          for (int q = 0; q < E; ++q) list[first + q] = x[q];
+        __syncthreads();
+      }
+      if (mine)
+#pragma unroll
+        for (int q = 0; q < E; ++q) {
+          const int at = first + q;
+          const Wide y = far ? list[at ^ j] : __shfl_xor_sync(0xFFFFFFFFu, x[q], j / E);
+          if (((at & j) == 0) == ((at & k) == 0) == (y > x[q])) x[q] = y;
+        }
     }
+#pragma unroll
+    for (int j = E / 2; j > 0; j /= 2)
+      if (j < k)
+#pragma unroll
+        for (int q = 0; q < E; ++q)
+          if ((q & j) == 0) {
+            const Wide u = x[q], v = x[q | j];
+            if ((u < v) == (((first + q) & k) == 0)) {
+              x[q] = v;
+              x[q | j] = u;
+            }
+          }
+  }
+  __syncthreads();
+  if (mine)
+#pragma unroll
+    for (int q = 0; q < E; ++q) list[first + q] = x[q];
+}
+// The block's list of n <= kList keys. Up to 128 by one warp: the others' turns at the loops of a sort that they have no part in
+// took most of its time (22 keys: 6,100 clocks by all, 900 by one).
+template <int kThreads>
+__device__ __noinline__ void sort_list(Wide* list, int n) {
+  __syncthreads();
+  if (n <= 128) {
+    if (threadIdx.x < 32) {
+      if (n <= 32) sort_short<1>(list, n);
+      else if (n <= 64) sort_short<2>(list, n);
+      else sort_short<4>(list, n);
+    }
+  } else if (n <= 256) {
+    sort_long<1>(list, n, 256);
+  } else if (n <= 512) {
+    sort_long<512 / kThreads>(list, n, 512);
+  } else {
+    sort_long<kList / kThreads>(list, n, kList);
+  }
+  __syncthreads();
 }
 
 // The scores of one load, with what is no number as -inf and of the two zeros one.
@@ -233,29 +310,6 @@ __device__ __noinline__ uint4 fetch_edge(const T* base, uint32_t at, uint32_t sh
 
 // ---- short rows ----
 
-// Keys of a warp, E neighbours a lane, descending.
-template <int E>
-__device__ __forceinline__ void sort_keys(Wide (&x)[E], int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32 * E; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2)
-#pragma unroll
-      for (int q = 0; q < E; ++q) {
-        const bool down = ((lane * E + q) & k) == 0;
-        if (j >= E) {
-          const Wide y = __shfl_xor_sync(0xFFFFFFFFu, x[q], j / E);
-          if ((((lane * E + q) & j) == 0) == down == (y > x[q])) x[q] = y;
-        } else if ((q & j) == 0) {
-          const Wide u = x[q], v = x[q | j];
-          if ((u < v) == down) {
-            x[q] = v;
-            x[q | j] = u;
-          }
-        }
-      }
-}
-
 struct Powers {
   double one;
   __device__ __forceinline__ double operator[](int i) const { return power(i, one); }
@@ -293,7 +347,7 @@ __device__ __noinline__ void short_row(const SampleArgs& a, int64_t p, const T* 
     Wide x[E];
 #pragma unroll
     for (int q = 0; q < E; ++q) x[q] = key(q);
-    sort_keys<E>(x, lane);
+    sort_warp<E>(x, lane);
     if (some) {
       Wide mine = 0;
 #pragma unroll
@@ -497,18 +551,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     s.least[warp] = low;
   }
   __syncthreads();
-  if (short_front && threadIdx.x < kParts) {
-    const float own = s.part[threadIdx.x];
-    int better = 0;
-#pragma unroll 8
-    for (int i = 0; i < kParts; i += 4) {
-      const float4 f = *reinterpret_cast<const float4*>(&s.part[i]);
-      better += f.x > own || (f.x == own && i < static_cast<int>(threadIdx.x));
-      better += f.y > own || (f.y == own && i + 1 < static_cast<int>(threadIdx.x));
-      better += f.z > own || (f.z == own && i + 2 < static_cast<int>(threadIdx.x));
-      better += f.w > own || (f.w == own && i + 3 < static_cast<int>(threadIdx.x));
-    }
-    if (better == share - 1) s.bound = own;
+  if (short_front && warp == 1) {
+    static_assert(kParts == 4 * 32, "four parts a lane");
+    const float4 f = *reinterpret_cast<const float4*>(&s.part[4 * lane]);
+    float x[4] = {f.x, f.y, f.z, f.w};
+    sort_warp<4>(x, lane);
+    const int at = share - 1;
+    if (lane == at / 4) s.bound = at % 4 == 0 ? x[0] : at % 4 == 1 ? x[1] : at % 4 == 2 ? x[2] : x[3];
   }
   if (warp == 0) {
     best = lane < kWarps ? s.warp[lane] : 0;
@@ -1103,7 +1152,7 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream, int64_t* launc
   constexpr int64_t kV = 16 / sizeof(T);
   const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
   // Short rows by a warp each: all of a call, or those of many segments or of segments that are short on the average, in a launch of
-  // their own (4,096 rows of 32 scores with top-k: 98 us by CTAs, 6.5 by warps; of 256 scores 98 and 26. Warps of the other
+  // their own (4,096 rows of 32 scores with top-k: 60 us by CTAs, 6 by warps; of 256 scores 60 and 26. Warps of the other
   // kernel's CTAs instead of a launch: no gain, its code grows).
   const bool all_short = a.c <= kShortRow, some_short = a.seg_off && (a.p >= kManyRows || len <= kShortRow);
   if (all_short || some_short) {
