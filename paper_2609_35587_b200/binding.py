@@ -145,26 +145,26 @@ def _dptr(t):
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _rows(t):
-    """Pointer and row stride (elements) of a matrix whose rows may be padded."""
+def _rows(t, device):
+    """Pointer and row stride (elements) of a matrix on the CUDA device of that index, whose rows may be padded."""
     rows, cols = t.shape
     ld, step = t.stride()
-    if not t.is_cuda or (cols > 1 and step != 1):
-        raise ValueError("expected a CUDA matrix with contiguous rows")
+    if t.get_device() != device or (cols > 1 and step != 1):
+        raise ValueError("expected a matrix with contiguous rows on the context's device")
     if cols == 0 or (rows <= 1 and ld < cols):  # (torch gives a single row, or rows without columns, any stride)
         ld = cols
     return t.data_ptr(), ld
 
 
-def _flat(t):
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError("expected a contiguous CUDA tensor")
+def _flat(t, device):
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError("expected a contiguous tensor on the context's device")
     return t.data_ptr()
 
 
-def _empty_e4m3(rows, cols, device):
-    """[rows, cols] e4m3 whose rows begin on 16-byte boundaries."""
-    wide = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn, device=device)
+def _empty_e4m3(t, rows, cols):
+    """[rows, cols] e4m3 on the device of t, whose rows begin on 16-byte boundaries."""
+    wide = t.new_empty((rows, (cols + 15) // 16 * 16), dtype=torch.float8_e4m3fn)
     return wide if cols % 16 == 0 else wide[:, :cols]
 
 
@@ -500,20 +500,21 @@ class Context:
         """Rows of fp32 / bf16 / fp16 values to e4m3 with a scale ("e8m0" or "f32") for each block of
         block_rows (1 or 128) x 128. Returns (q, scales); the rows of q begin on 16-byte boundaries."""
         rows, cols = x.shape
+        dev = self.device.index
+        xp, ldx = _rows(x, dev)
         st, dtype = _SCALES[scale]
         blocks = (-(-rows // max(int(block_rows), 1)), (cols + 127) // 128)  # an invalid one is reported by the library, not by torch
         if out is None:
-            out = _empty_e4m3(rows, cols, self.device)
+            out = _empty_e4m3(x, rows, cols)
         elif out.shape != x.shape or out.dtype != torch.float8_e4m3fn:
             raise ValueError("quantize_e4m3: out")
         if out_scale is None:
-            out_scale = torch.empty(blocks, dtype=dtype, device=self.device)
+            out_scale = x.new_empty(blocks, dtype=dtype)
         elif out_scale.shape != blocks or out_scale.dtype != dtype:
             raise ValueError("quantize_e4m3: out_scale")
-        xp, ldx = _rows(x)
-        qp, ldq = _rows(out)
+        qp, ldq = _rows(out, dev)
         status = _lib.ks_quantize_e4m3(self._h, xp, _TYPES.get(x.dtype, -1), rows, cols, ldx, int(block_rows), st, qp, ldq,
-                                       _flat(out_scale), _raw_stream(self.device.index))
+                                       _flat(out_scale, dev), _raw_stream(dev))
         if status:
             self._check(status, "ks_quantize_e4m3")
         return out, out_scale
@@ -534,20 +535,21 @@ class Context:
         if bias is not None and (bias.dtype != torch.float32 or bias.shape != (n,)):
             raise ValueError("matmul_e4m3: bias")
         quantised = out_dtype == e4m3
+        dev = self.device.index
+        ap, lda = _rows(a, dev)
+        bp, ldb = _rows(b, dev)
         if out is None:
-            out = _empty_e4m3(m, n, self.device) if quantised else torch.empty((m, n), dtype=out_dtype, device=self.device)
+            out = _empty_e4m3(a, m, n) if quantised else a.new_empty((m, n), dtype=out_dtype)
         elif out.shape != (m, n) or out.dtype != out_dtype:
             raise ValueError("matmul_e4m3: out")
         if quantised and out_scale is None:
-            out_scale = torch.empty((m, (n + 127) // 128), dtype=scales, device=self.device)
+            out_scale = a.new_empty((m, (n + 127) // 128), dtype=scales)
         elif out_scale is not None and (not quantised or out_scale.dtype != scales or out_scale.shape != (m, (n + 127) // 128)):
             raise ValueError("matmul_e4m3: out_scale")
-        ap, lda = _rows(a)
-        bp, ldb = _rows(b)
-        op, ldd = _rows(out)
-        status = _lib.ks_matmul_e4m3(self._h, ap, lda, _flat(a_scale), bp, ldb, _flat(b_scale), _SCALE_TYPES[scales], m, n, k,
-                                     None if bias is None else _flat(bias), int(relu), op, ldd, _TYPES.get(out_dtype, -1),
-                                     _flat(out_scale) if quantised else None, _raw_stream(self.device.index))
+        op, ldd = _rows(out, dev)
+        status = _lib.ks_matmul_e4m3(self._h, ap, lda, _flat(a_scale, dev), bp, ldb, _flat(b_scale, dev), _SCALE_TYPES[scales],
+                                     m, n, k, None if bias is None else _flat(bias, dev), int(relu), op, ldd,
+                                     _TYPES.get(out_dtype, -1), _flat(out_scale, dev) if quantised else None, _raw_stream(dev))
         if status:
             self._check(status, "ks_matmul_e4m3")
         return (out, out_scale) if quantised else out
@@ -559,31 +561,32 @@ class Context:
         instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each; with an
         out_idx and no out_logp the second is None and not computed."""
         P, draws = u.shape
+        dev = self.device.index
+        up = _flat(u, dev)
         if u.dtype != torch.float32 or scores.dtype not in _TYPES:
             raise ValueError("sample: element types")
         if d_seg_off is None:
             if scores.shape[0] != P:
                 raise ValueError("sample: a row of scores for each row of u")
-            sp, ld = _rows(scores)
+            sp, ld = _rows(scores, dev)
             c, off = scores.shape[1], None
         else:
             if d_seg_off.dtype != torch.int64 or d_seg_off.shape != (P + 1,):
                 raise ValueError("sample: d_seg_off")
-            sp, ld, c, off = _flat(scores), 0, scores.numel(), _flat(d_seg_off)
+            sp, ld, c, off = _flat(scores, dev), 0, scores.numel(), _flat(d_seg_off, dev)
         if params is not None and params.numel() * params.element_size() != 16 * P:
             raise ValueError("sample: params")
         if out_idx is None:
-            out_idx = torch.empty((P, draws), dtype=torch.int32, device=self.device)
+            out_idx = u.new_empty((P, draws), dtype=torch.int32)
             if out_logp is None:
-                out_logp = torch.empty((P, draws), dtype=torch.float32, device=self.device)
+                out_logp = u.new_empty((P, draws))
         elif out_idx.shape != u.shape or out_idx.dtype != torch.int32:
             raise ValueError("sample: out_idx")
         if out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32):
             raise ValueError("sample: out_logp")
         one = None if params is not None else ctypes.byref(_Sampling(temperature, top_k, top_p, min_p))
-        status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params),
-                                _flat(u), draws, _flat(out_idx), None if out_logp is None else _flat(out_logp),
-                                _raw_stream(self.device.index))
+        status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params, dev),
+                                up, draws, _flat(out_idx, dev), None if out_logp is None else _flat(out_logp, dev), _raw_stream(dev))
         if status:
             self._check(status, "ks_sample")
         return out_idx, out_logp

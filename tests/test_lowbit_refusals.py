@@ -4,6 +4,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from paper_2609_35587_b200 import binding as ks
 
@@ -112,3 +113,16 @@ def test_model_in_eight_bits():
     assert create(7, widths) == ks.KS_ERR_INVALID_ARG
     assert create(2, widths, np.zeros(64, np.float32)) == ks.KS_ERR_INVALID_ARG
     assert out.value is None
+
+
+def test_binding_wants_the_context_device():
+    """Tensors in host memory or on another GPU are not handed over."""
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 1
+    there = torch.zeros(2, 4).as_subclass(Elsewhere)
+    for fn in (ks._rows, ks._flat):
+        for t in (torch.zeros(2, 4), there):
+            with pytest.raises(ValueError):
+                fn(t, 0)
+        assert fn(there, 1)
