@@ -16,14 +16,14 @@
 // A short front (top-k of some hundred) needs no histogram: the k-th largest of the maxima of 128 parts of the row bounds the
 // k-th score from below, so that little more than k candidates are listed, sorted, cut, and drawn from in the list.
 //
-// A row of a call with few rows belongs to a cluster of up to 16 CTAs that keep its scores in shared memory, each thread its
-// own; the CTAs' results meet there too. Where there are rows for the whole machine a CTA takes a row by itself: short ones are
-// kept, by four CTAs an SM, long ones read again in every phase by two CTAs an SM, which is what stays in L2 (1,024 x 60,000
-// scores with top-k 50: 298 us by four CTAs, 217 by two; with top-p 0.95 as it was then 416 and 410, by clusters of four 947).
+// A row of a call with few rows belongs to a cluster of up to 16 CTAs, each with a stretch of it; their results meet in shared
+// memory. Where there are rows for the whole machine a CTA takes a row by itself. Stretches that fit are kept in shared memory
+// (short rows by four CTAs an SM), others read again in every phase by two CTAs an SM, which is what stays in L2. Rows of up to
+// 256 scores belong to a warp each (short_rows_kernel).
 //
-// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 365 us where reading them takes 38: three passes, of
-// which the one with the weights (20 operations in 64 bits and the sums) takes half; the issue slots are 67 % busy, the fp64
-// pipe 13 %. Single rows are bound by the clusters' meetings: 60,000 scores with top-k and top-p 15 us.
+// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 360 us where reading them takes 38: three passes, of
+// which the one with the weights (20 operations in 64 bits and the sums) takes half; the issue slots are 66 % busy, the fp64
+// pipe 12 %. With top-k 50 113 us. Few rows are bound by the phases' latency: one of 60,000 scores 12 us with top-k, 33 with top-p.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -1171,13 +1171,14 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream, int64_t* launc
       return launch_as<T, kSmall>(a, 1, static_cast<int>(a.seg_off ? kKept : std::min(kKept, (len + 64 * kV) / (kSmall * kV) + 1)), done, stream);
     return launch_as<T, kLarge>(a, 1, 0, done, stream);
   }
+  // Few rows: a cluster each, while all of its CTAs can run at once (two an SM; clusters of 16 on half of that) and have 5,000 scores and
+  // more. 64 x 131,072 fp32 scores, top-p: 81 us by 4 CTAs a row, 123 by 8, in two waves, that keep their scores; 290 x 60,000: 104 by
+  // one, 138 by 2, 213 by 4; 8 x 8,192, top-k: 10 by one, 11 by 2 or 4, 20 by 8.
   int ctas = 1;
-  while (ctas < kMaxCtas && kLarge * kV * kHeldLoads * ctas < len) ctas *= 2;
-  // few rows: more CTAs each, while they have a thousand scores and more
-  while (ctas < kMaxCtas && a.p * ctas * 2 <= 148 && len / (2 * ctas) >= 1024) ctas *= 2;
-  if (a.p * ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+  while (ctas < kMaxCtas && a.p * ctas * 2 <= (ctas < 8 ? 296 : 148) && len / (2 * ctas) >= 5000) ctas *= 2;
   const int64_t each = (a.seg_off ? 2 * len : len + ctas - 1) / ctas + 64 * kV;
-  const int64_t loads = std::min<int64_t>(kHeldLoads, (each + kLarge * kV - 1) / (kLarge * kV));
+  int64_t loads = (each + kLarge * kV - 1) / (kLarge * kV);
+  if (loads > kHeldLoads) loads = a.seg_off ? kHeldLoads : 0;
   return launch_as<T, kLarge>(a, ctas, static_cast<int>(loads), done, stream);
 }
 
