@@ -243,7 +243,7 @@ __device__ __forceinline__ void sort_long(Wide* list, int n, int size) {
     for (int q = 0; q < E; ++q) list[first + q] = x[q];
 }
 // The block's list of n <= kList keys. Up to 128 by one warp: the others' turns at the loops of a sort that they have no part in
-// took most of its time (22 keys: 6,100 clocks by all, 900 by one).
+// took most of its time (22 keys: 6,100 clocks by all, about 1,100 by one).
 template <int kThreads>
 __device__ __noinline__ void sort_list(Wide* list, int n) {
   __syncthreads();
