@@ -10,8 +10,9 @@
 // lie; they are sorted. Bins that hold more are narrowed down further by the bits of (score, index).
 //
 // The sums of weights that top-p's histogram needs are first estimated in 32 bits; one pass with the weights themselves then
-// sums up what lies surely in front of the cut and lists the candidates of the few bins around it, which are sorted. Where the
-// estimate was not good enough the exact histogram is made.
+// sums up what lies surely in front of the cut and lists the candidates of the few bins around it, which are sorted. Bins that
+// hold more than a list are estimated again in 1,024 bins of their own (64 x 500,000 scores: 659 us without, 257 so). Where
+// the estimate was not good enough, or candidates share a score, the exact histogram is made.
 //
 // A short front (top-k of some hundred) needs no histogram: the k-th largest of the maxima of 128 parts of the row bounds the
 // k-th score from below, so that little more than k candidates are listed, sorted, cut, and drawn from in the list.
@@ -21,7 +22,7 @@
 // (short rows by four CTAs an SM), others read again in every phase by two CTAs an SM, which is what stays in L2. Rows of up to
 // 256 scores belong to a warp each (short_rows_kernel).
 //
-// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 360 us where reading them takes 38: three passes, of
+// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 350 us where reading them takes 38: three passes, of
 // which the one with the weights (20 operations in 64 bits and the sums) takes half; the issue slots are 66 % busy, the fp64
 // pipe 12 %. With top-k 50 113 us. Few rows are bound by the phases' latency: one of 60,000 scores 12 us with top-k, 33 with top-p.
 #include <algorithm>
@@ -146,7 +147,7 @@ struct Shared {
   Wide best;
   float least[kWarps], min, bound;
   alignas(16) float part[kParts];
-  Wide share, before, total, cut, front;
+  Wide share, before, total, cut, front, window[2];
   int bin, first_bin, last_bin;
   unsigned listed;
 };
@@ -859,81 +860,123 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   bool summed = false;   // they are there
   // The cut of top-p by an estimate; false: it did not serve.
   auto estimated_cut = [&](double part) KS_INLINE -> bool {
-    for (int i = threadIdx.x; i < kBins; i += kThreads) s.low[i] = s.high[i] = 0;
-    if (threadIdx.x == 0) s.listed = 0;
-    __syncthreads();
     const float octaves = 1.4426950408889634f / set.temperature;
     const bool cuts = cut_score > none;  // an earlier cut leaves some
-    each_load(std::true_type{}, [&](uint32_t i, const float (&y)[V]) KS_INLINE {
-      unsigned add[V], d[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        // The weight times 2^30 (with 2^22, which needs no conversion, 16-bit scores that share a value are all rounded the same
-        // way, and the estimate failed for one row in 20). The relative error of 53 octaves in fp32 is below 2^-18. What is no
-        // number, or -inf, adds 0.
-        const float below = y[v] - r.best;
-        float w;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(below * octaves));
-        add[v] = __float2uint_rn(w * 1073741824.0f);
-        d[v] = __float_as_uint(fminf(-below * r.bins, static_cast<float>(kBins - 1)) + 8388608.0f) & (kBins - 1);
-      }
-      if (cuts)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (!inside(i + v, y[v])) add[v] = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (add[v] > 0) {
-          const unsigned was = atomicAdd(&s.low[d[v]], add[v]);
-          if (was + add[v] < was) atomicAdd(&s.high[d[v]], 1u);
-        }
-    });
-    meet(ctas);
-    Wide own = 0, share;
-    for (int i = threadIdx.x; i < mine; i += kThreads) {
-      Wide b = 0;
-      if (ctas == 1) {
-        b = bin_sum(i);
-      } else {
-        for (int o = 0; o < ctas; ++o)
-          b += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
-        s.merged[i] = b;
-      }
-      own += b;
-    }
-    block_scan(own, s.warp, share);
-    if (threadIdx.x == 0) s.share = share;
-    meet(ctas);
-    Wide before = 0, all = 0;
-    for (int o = 0; o < ctas; ++o) {
-      const Wide t = *of_rank(&s.share, o, ctas);
-      if (o < rank) before += t;
-      all += t;
-    }
-    // the bins in which the sum reaches a little less and a little more than the part
-    const double goal = part * static_cast<double>(all);
-    const Wide least = static_cast<Wide>(goal * (1.0 - 1.0 / 8192)), most = min(all, static_cast<Wide>(goal * (1.0 + 1.0 / 8192)) + 1);
-    if (threadIdx.x == 0) s.first_bin = s.last_bin = -1;
-    Wide mine_sum = 0, total;
-    for (int q = 0; q < per; ++q)
-      if (static_cast<int>(threadIdx.x) * per + q < mine) mine_sum += bin_sum(threadIdx.x * per + q);
-    Wide b = block_scan(mine_sum, s.warp, total) + before;
-    for (int q = 0; q < per && static_cast<int>(threadIdx.x) * per + q < mine; ++q) {
-      const int i = threadIdx.x * per + q;
-      const Wide e = b + bin_sum(i);
-      if (b <= least && e > least) s.first_bin = rank * mine + i;
-      if (b < most && e >= most) s.last_bin = rank * mine + i;
-      b = e;
-    }
-    meet(ctas);
+    // The bins [first0, last0] of the first histogram, where they hold more candidates than can be listed, in bins of their own.
+    bool fine = false;
+    int first0 = 0, last0 = 0;
+    float origin = 0.0f, scale = 0.0f;
+    auto fine_bin = [&](float y, int d) KS_INLINE {
+      const float f = fminf(fmaxf((r.best - y - origin) * scale, 0.0f), static_cast<float>(kBins - 1));
+      return d < first0 ? -1 : d > last0 ? kBins : static_cast<int>(f);
+    };
+    Wide all = 0, base = 0;
     int first_bin = -1, last_bin = -1;
-    for (int o = 0; o < ctas; ++o) {
-      first_bin = max(first_bin, *of_rank(&s.first_bin, o, ctas));
-      last_bin = max(last_bin, *of_rank(&s.last_bin, o, ctas));
-    }
-    if (first_bin < 0 || last_bin < 0) {  // (all threads find the same)
+    for (;;) {
+      for (int i = threadIdx.x; i < kBins; i += kThreads) s.low[i] = s.high[i] = 0;
+      if (threadIdx.x == 0) s.listed = 0;
+      __syncthreads();
+      auto estimate = [&](auto is_fine) KS_INLINE {
+        each_load(std::true_type{}, [&](uint32_t i, const float (&y)[V]) KS_INLINE {
+          unsigned add[V];
+          int d[V];
+#pragma unroll
+          for (int v = 0; v < V; ++v) {
+            // The weight times 2^30 (with 2^22, which needs no conversion, 16-bit scores that share a value are all rounded the same
+            // way, and the estimate failed for one row in 20). The relative error of 53 octaves in fp32 is below 2^-18. What is no
+            // number, or -inf, adds 0.
+            const float below = y[v] - r.best;
+            float w;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(below * octaves));
+            add[v] = __float2uint_rn(w * 1073741824.0f);
+            d[v] = __float_as_uint(fminf(-below * r.bins, static_cast<float>(kBins - 1)) + 8388608.0f) & (kBins - 1);
+          }
+          if (cuts)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+              if (!inside(i + v, y[v])) add[v] = 0;
+          if constexpr (decltype(is_fine)::value) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              d[v] = fine_bin(y[v], d[v]);
+              if (d[v] < 0 || d[v] >= kBins) add[v] = 0;
+            }
+          }
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+            if (add[v] > 0) {
+              const unsigned was = atomicAdd(&s.low[d[v]], add[v]);
+              if (was + add[v] < was) atomicAdd(&s.high[d[v]], 1u);
+            }
+        });
+      };
+      if (fine) estimate(std::true_type{});
+      else estimate(std::false_type{});
       meet(ctas);
-      return false;
+      Wide own = 0, share;
+      for (int i = threadIdx.x; i < mine; i += kThreads) {
+        Wide b = 0;
+        if (ctas == 1) {
+          b = bin_sum(i);
+        } else {
+          for (int o = 0; o < ctas; ++o)
+            b += (static_cast<Wide>(*of_rank(&s.high[rank * mine + i], o, ctas)) << 32) + *of_rank(&s.low[rank * mine + i], o, ctas);
+          s.merged[i] = b;
+        }
+        own += b;
+      }
+      block_scan(own, s.warp, share);
+      if (threadIdx.x == 0) s.share = share;
+      meet(ctas);
+      Wide before = base;
+      for (int o = 0; o < ctas; ++o) {
+        const Wide t = *of_rank(&s.share, o, ctas);
+        if (o < rank) before += t;
+        if (!fine) all += t;
+      }
+      // the bins in which the sum reaches a little less and a little more than the part
+      const double goal = part * static_cast<double>(all);
+      const Wide least = static_cast<Wide>(goal * (1.0 - 1.0 / 8192)), most = min(all, static_cast<Wide>(goal * (1.0 + 1.0 / 8192)) + 1);
+      if (threadIdx.x == 0) s.first_bin = s.last_bin = -1;
+      Wide mine_sum = 0, total;
+      for (int q = 0; q < per; ++q)
+        if (static_cast<int>(threadIdx.x) * per + q < mine) mine_sum += bin_sum(threadIdx.x * per + q);
+      Wide b = block_scan(mine_sum, s.warp, total) + before;
+      for (int q = 0; q < per && static_cast<int>(threadIdx.x) * per + q < mine; ++q) {
+        const int i = threadIdx.x * per + q;
+        const Wide e = b + bin_sum(i);
+        if (b <= least && e > least) {
+          s.first_bin = rank * mine + i;
+          if (!fine) s.window[0] = b;
+        }
+        if (b < most && e >= most) {
+          s.last_bin = rank * mine + i;
+          if (!fine) s.window[1] = e;
+        }
+        b = e;
+      }
+      meet(ctas);
+      first_bin = last_bin = -1;
+      Wide up_to = 0;
+      for (int o = 0; o < ctas; ++o) {
+        const int f = *of_rank(&s.first_bin, o, ctas), l = *of_rank(&s.last_bin, o, ctas);
+        first_bin = max(first_bin, f);
+        last_bin = max(last_bin, l);
+        if (!fine && f >= 0) base = *of_rank(&s.window[0], o, ctas);
+        if (!fine && l >= 0) up_to = *of_rank(&s.window[1], o, ctas);
+      }
+      if (first_bin < 0 || last_bin < 0) {  // (all threads find the same)
+        meet(ctas);
+        return false;
+      }
+      // no more candidates than their sum has of the least of their weights (the last bin has no end)
+      const float end = (static_cast<float>(last_bin) + 0.5f) / r.bins, lightest = exp2f(-end * octaves) * 1073741824.0f;
+      if (fine || last_bin == kBins - 1 || static_cast<float>(up_to - base) <= kList * lightest) break;
+      fine = true;
+      first0 = first_bin;
+      last0 = last_bin;
+      origin = (static_cast<float>(first_bin) - 0.5f) / r.bins;
+      scale = kBins * r.bins / static_cast<float>(last_bin - first_bin + 1);
     }
     // the weights: of all, of what lies in front of those bins (by stretches what min-p lets stay), and who lies in them
     unsigned* n_list = of_rank(&s.listed, 0, ctas);
@@ -941,39 +984,44 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     ends = reinterpret_cast<Wide*>(s.low);
     const bool least_counts = r.least > 0.0;
     Wide sum = 0, front = 0;
-    for (int tile = 0; tile < tiles; ++tile) {
-      Wide stretch = 0;
-      uint32_t at = place(tile, warp, 0);
-      const uint32_t lane0 = at - lane * V;
-      const int steps = lane0 >= last ? 0 : min(loads, static_cast<int>((last - lane0 + 32 * V - 1) / (32 * V)));
-      uint4 next = make_uint4(0, 0, 0, 0);
-      if (steps > 0) next = get(at, warp, 0);
+    auto weigh = [&](auto is_fine) KS_INLINE {
+      for (int tile = 0; tile < tiles; ++tile) {
+        Wide stretch = 0;
+        uint32_t at = place(tile, warp, 0);
+        const uint32_t lane0 = at - lane * V;
+        const int steps = lane0 >= last ? 0 : min(loads, static_cast<int>((last - lane0 + 32 * V - 1) / (32 * V)));
+        uint4 next = make_uint4(0, 0, 0, 0);
+        if (steps > 0) next = get(at, warp, 0);
 #pragma unroll 1
-      for (int q = 0; q < steps; ++q, at += 32 * V) {
-        float y[V];
-        unpack_as_is<T, V>(next, y);
-        if (q + 1 < steps) next = get(at + 32 * V, warp, q + 1);
+        for (int q = 0; q < steps; ++q, at += 32 * V) {
+          float y[V];
+          unpack_as_is<T, V>(next, y);
+          if (q + 1 < steps) next = get(at + 32 * V, warp, q + 1);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const double exact = scaled_weight(r, s.table, y[v]);
-          bool in = r.best - y[v] <= r.reach;  // (not so of what is no number)
-          if (cuts) in = in && inside(at + v, y[v]);
-          const Wide w = in ? whole(exact) : 0;
-          const int bin = bin_of(r, y[v]);
-          sum += w;
-          if (bin < first_bin) {
-            if (!least_counts) stretch += w;
-            else front += w, stretch += exact >= r.least ? w : 0;
-          } else if (bin <= last_bin && w > 0) {
-            const unsigned to = atomicAdd(n_list, 1u);
-            if (to < kList) list[to] = key_of(at + v, normal(y[v]));
+          for (int v = 0; v < V; ++v) {
+            const double exact = scaled_weight(r, s.table, y[v]);
+            bool in = r.best - y[v] <= r.reach;  // (not so of what is no number)
+            if (cuts) in = in && inside(at + v, y[v]);
+            const Wide w = in ? whole(exact) : 0;
+            int bin = bin_of(r, y[v]);
+            if constexpr (decltype(is_fine)::value) bin = fine_bin(y[v], bin);
+            sum += w;
+            if (bin < first_bin) {
+              if (!least_counts) stretch += w;
+              else front += w, stretch += exact >= r.least ? w : 0;
+            } else if (bin <= last_bin && w > 0) {
+              const unsigned to = atomicAdd(n_list, 1u);
+              if (to < kList) list[to] = key_of(at + v, normal(y[v]));
+            }
           }
         }
+        if (!least_counts) front += stretch;
+        stretch = warp_sum(stretch);
+        if (lane == 0) ends[tile * kWarps + warp] = stretch;
       }
-      if (!least_counts) front += stretch;
-      stretch = warp_sum(stretch);
-      if (lane == 0) ends[tile * kWarps + warp] = stretch;
-    }
+    };
+    if (fine) weigh(std::true_type{});
+    else weigh(std::false_type{});
     Wide block_sum, block_front;
     block_scan(sum, s.warp, block_sum);
     block_scan(front, s.warp, block_front);
@@ -1002,7 +1050,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
           w[q] = i >= listed ? 0 : weight(key_score(s.list[i]));
           sum += w[q];
         }
-        Wide e = block_scan(sum, s.warp, total) + front;
+        Wide total, e = block_scan(sum, s.warp, total) + front;
 #pragma unroll
         for (int q = 0; q < kEach; ++q) {
           if (e < target && e + w[q] >= target) s.cut = s.list[threadIdx.x * kEach + q];

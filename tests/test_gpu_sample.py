@@ -270,3 +270,16 @@ def test_short_rows(ctx, c, dtype, s):
     lens = torch.tensor([0] + [c, 3000] * few, dtype=torch.int64)
     seg = draw(ctx, flat, u[:few].repeat_interleave(2, 0).contiguous(), seg_off=lens.cumsum(0).to(DEV), **s)
     assert torch.equal(seg[0][::2], idx[:few]) and torch.equal(seg[1][::2], logp[:few])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("p,c", [(1, 400000), (20, 200000), (300, 130000)])
+@pytest.mark.parametrize("s", [dict(top_p=0.9), dict(top_p=0.3, t=0.8, min_p=0.001), dict(top_k=100000, top_p=0.8), dict(top_p=0.999, t=2.0)], ids=str)
+@pytest.mark.parametrize("spread", [0.05, 1.0, 3.0])
+def test_many_scores_around_the_cut(ctx, p, c, dtype, s, spread):
+    """Long rows in which a bin of the histogram around top-p's cut holds more candidates than are listed."""
+    x = (torch.randn(p, c, generator=torch.Generator(device=DEV).manual_seed(c), device=DEV) * spread).to(dtype)
+    u = numbers(p, 4, 3)
+    idx, logp = draw(ctx, x, u, **s)
+    for r in ([0] if p == 1 else [0, p - 1]):
+        lowbit.check_draws(lowbit.as_float64(x[r]), u[r].cpu().numpy(), idx[r].cpu().numpy(), logp[r].cpu().numpy(), **s)
