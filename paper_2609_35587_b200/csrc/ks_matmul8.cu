@@ -4,7 +4,7 @@
 // is plain, so that the scales come in once per block. A tensor core makes a block's sums (128 of K, four MMAs of 32) into one
 // of two accumulators, the epilogue's threads read them and add them, scaled, to fp32 sums in their registers, while the other
 // accumulator is filled. So the sums of blocks are added with rounding, not with the tensor core's truncation, and scales of
-// any value cost the same (matmul_pair_kernel; matmul_few_kernel for up to 64 rows). Scales that are powers of two the tensor
+// any value cost the same (matmul_pair_kernel; matmul_few_kernel for few results). Scales that are powers of two the tensor
 // core multiplies in, and a long sum is read once (matmul_scaled_kernel).
 #include <cuda.h>
 
@@ -826,6 +826,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int part = static_cast<int>(blockIdx.x) % parts, n0 = static_cast<int>(blockIdx.x) / parts * kScaleBlock;
+  const int m0 = static_cast<int>(blockIdx.y) * kN;
   const int kb0 = static_cast<int>(static_cast<int64_t>(p.kblocks) * part / parts);
   const int kb1 = static_cast<int>(static_cast<int64_t>(p.kblocks) * (part + 1) / parts);
   unsigned char* smem = smem_raw + ((1024u - (smem_addr(smem_raw) & 1023u)) & 1023u);
@@ -883,7 +884,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
         bar_expect(bar_full(s), kFewStageBytes<kN>);
         if (p.starve) continue;
         load_one(sbase + s * kFewStageBytes<kN>, &map_b, kb * kScaleBlock, n0, bar_full(s));
-        load_one(sbase + s * kFewStageBytes<kN> + kOperandBytes, &map_a, kb * kScaleBlock, 0, bar_full(s));
+        load_one(sbase + s * kFewStageBytes<kN> + kOperandBytes, &map_a, kb * kScaleBlock, m0, bar_full(s));
       }
     }
     __syncwarp();
@@ -907,13 +908,13 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
     // The scales' products: threads by row and by stretches of a chunk, once for the four warps that use them (each of which
     // fetching its own took 28 us where this takes 20: 64 rows by 8,192 x 8,192, fp32 scales)
     constexpr int kOf = kN * kChunk / 64;  // blocks of a thread
-    const int t = threadIdx.x - 64, r = t % kN, first = t / kN * kOf;
-    const int64_t sa_at = static_cast<int64_t>(r < p.m ? r : 0) * p.kblocks, sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
+    const int t = threadIdx.x - 64, r = t % kN, first = t / kN * kOf, m = m0 + r;
+    const int64_t sa_at = static_cast<int64_t>(m < p.m ? m : 0) * p.kblocks, sb_at = static_cast<int64_t>(n0 / kScaleBlock) * p.kblocks;
     for (int kb = kb0, it = 0; kb < kb1; kb += kChunk, ++it) {
       float v[kOf];
 #pragma unroll
       for (int k = 0; k < kOf; ++k)
-        v[k] = r < p.m && kb + first + k < kb1 ? scale_value(p.a_scale, sa_at + kb + first + k, p.scale_type) *
+        v[k] = m < p.m && kb + first + k < kb1 ? scale_value(p.a_scale, sa_at + kb + first + k, p.scale_type) *
                                                      scale_value(p.b_scale, sb_at + kb + first + k, p.scale_type) : 0.0f;
       if (!__all_sync(0xFFFFFFFFu, wait_ok(bar_used(it & 1), ((it >> 1) & 1u) ^ 1u))) break;
 #pragma unroll
@@ -978,7 +979,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
   __syncthreads();
   if (parts > 1) cluster_sync();
   // rows of the result, dealt among the cluster's warps; a warp adds the parts of 128 columns, a lane four neighbours
-  const int rows = p.m;
+  const int rows = min(p.m - m0, kN);
   const int n = n0 + 4 * lane;
   if (!*v_fail)
     for (int r = part * (kFewThreads / 32) + warp; r < rows; r += parts * (kFewThreads / 32)) {
@@ -999,7 +1000,7 @@ matmul_few_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__ 
         v[e] = n + e < p.n ? finish(p, v[e], n + e) : 0.0f;
         amax = fmaxf(amax, finite_abs(v[e]));
       }
-      const int64_t row = r;
+      const int64_t row = m0 + r;
       if (kType == KS_E4M3) {
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, d));
@@ -1072,20 +1073,23 @@ cudaError_t launch_few(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t st
   const void* kernel = reinterpret_cast<const void*>(&matmul_few_kernel<kType, kN>);
   if (e == cudaSuccess) e = ensure_dynamic_smem(kernel, kFewSmem<kN>);
   if (e != cudaSuccess) return e;
-  const int64_t tiles = scale_blocks(q.n);  // (below 2^24)
+  const int64_t tiles = scale_blocks(q.n), rows = (q.m + kN - 1) / kN;  // (below 2^24; launch_type gives few)
   // parts of K, so that the machine's CTAs have work each
   int parts = 1;
-  while (parts < 8 && 2 * parts <= p.kblocks && tiles * parts * 2 <= kSms * 2) parts *= 2;
-  return launch_following(&matmul_few_kernel<kType, kN>, dim3(static_cast<unsigned>(tiles * parts)), kFewThreads,
+  while (parts < 8 && 2 * parts <= p.kblocks && tiles * rows * parts * 2 <= kSms * 2) parts *= 2;
+  return launch_following(&matmul_few_kernel<kType, kN>, dim3(static_cast<unsigned>(tiles * parts), static_cast<unsigned>(rows)), kFewThreads,
                           kFewSmem<kN>, parts, stream, p, ma, mb, parts);
 }
 
 template <int kType>
 cudaError_t launch_type(const MatmulE4m3& q, const MatmulArgs& p, cudaStream_t stream) {
-  // (65 and 128 rows by 8,192 x 8,192: 41 and 47 us by columns of 128, 34 and 35 by pairs; 64 rows 24 and 34)
   if (q.m <= 16) return launch_few<kType, 16>(q, p, stream);
   if (q.m <= 32) return launch_few<kType, 32>(q, p, stream);
-  if (q.m <= 64) return launch_few<kType, 64>(q, p, stream);
+  // Many rows too, where their results are so few that pairs would leave most of the machine idle (K is shared out there): K = 8,192,
+  // 128 x 1,024 results with powers of two 25 us by pairs, 12 so, 512 x 1,024 26 and 19, 512 x 2,048 26 and 28. Pairs are slower
+  // with fp32 scales: K = 8,192, 512 x 2,048 34 and 28, 512 x 4,096 34 and 48; K = 512, 512 x 2,048 7.7 and 8.4.
+  const int64_t few = q.scale_type == KS_SCALE_F32 && p.kblocks >= 16 ? 128 : 64;
+  if (q.m <= 64 || (q.m <= 64 * few && (q.m + 63) / 64 * scale_blocks(q.n) <= few)) return launch_few<kType, 64>(q, p, stream);
   return q.scale_type == KS_SCALE_E8M0 ? launch_pair<kType, true>(q, p, stream) : launch_pair<kType, false>(q, p, stream);
 }
 

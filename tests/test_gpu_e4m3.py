@@ -107,7 +107,7 @@ def off_by(k, mag, want, dtype):
 
 SHAPES = [(1, 1, 1), (1, 128, 128), (1, 1000, 4096), (7, 130, 129), (16, 512, 1000), (17, 64, 640), (33, 300, 77), (64, 384, 2048),
           (65, 129, 128), (128, 256, 256), (129, 255, 300), (200, 1024, 1024), (256, 512, 384), (300, 700, 500), (513, 257, 129),
-          (1025, 1100, 520)]
+          (1025, 1100, 520), (4200, 130, 300), (1300, 520, 2100), (2100, 520, 2100)]
 
 
 @pytest.mark.parametrize("scale", ["e8m0", "f32"])
@@ -121,7 +121,7 @@ def test_matmul(ctx, m, n, k, scale):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("m,n,k", [(1, 300, 256), (48, 1000, 700), (100, 130, 256), (300, 500, 700)])
+@pytest.mark.parametrize("m,n,k", [(1, 300, 256), (48, 1000, 700), (100, 130, 256), (300, 500, 700), (4200, 130, 256), (1100, 600, 700)])
 def test_matmul_epilogue(ctx, m, n, k, dtype):
     """Bias, ReLU, each result type, a result with padded rows of which nothing else is written."""
     (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, n, k, "f32", 5)
@@ -143,7 +143,7 @@ def test_matmul_epilogue(ctx, m, n, k, dtype):
 
 
 @pytest.mark.parametrize("scale", ["e8m0", "f32"])
-@pytest.mark.parametrize("m,n,k", [(1, 256, 256), (5, 129, 300), (64, 1000, 512), (130, 128, 128), (300, 450, 1024)])
+@pytest.mark.parametrize("m,n,k", [(1, 256, 256), (5, 129, 300), (64, 1000, 512), (130, 128, 128), (300, 450, 1024), (4200, 130, 300), (1200, 450, 1024)])
 def test_matmul_quantised_result(ctx, m, n, k, scale):
     (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, n, k, scale, 9)
     sums, mag = lowbit.matmul(av, sav, bv, sbv)
@@ -165,7 +165,7 @@ def test_matmul_quantised_result(ctx, m, n, k, scale):
     assert bool((wide[m:] == 0x55).all()) and bool((wide[:, n:] == 0x55).all())
 
 
-@pytest.mark.parametrize("m", [3, 300])
+@pytest.mark.parametrize("m", [3, 300, 4200])
 @pytest.mark.parametrize("scale", [torch.float32, torch.float8_e8m0fnu])
 def test_matmul_empty_sum_of_many_rows(ctx, m, scale):
     a, b = torch.empty(m, 0, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(130, 0, dtype=torch.float8_e4m3fn, device=DEV)
@@ -185,7 +185,7 @@ def test_matmul_empty_sum(ctx):
     assert torch.equal(got, bias.clamp(min=0).expand(3, 130))
 
 
-@pytest.mark.parametrize("m", [3, 200])
+@pytest.mark.parametrize("m", [3, 200, 4200])
 @pytest.mark.parametrize("scale", ["e8m0", "f32"])
 def test_matmul_not_a_number(ctx, m, scale):
     """A code that is no number spoils its row (a) or column (b) and nothing else; ReLU makes 0 of it."""
@@ -202,10 +202,11 @@ def test_matmul_not_a_number(ctx, m, scale):
     assert (got[spoiled] == 0).all()
 
 
+@pytest.mark.parametrize("m", [40, 4200])
 @pytest.mark.parametrize("scale", ["e8m0", "f32"])
-def test_matmul_extreme_scales(ctx, scale):
+def test_matmul_extreme_scales(ctx, scale, m):
     """Scales far from one whose product is an ordinary number."""
-    (a, sa, av, sav), (b, sb, bv, sbv) = operands(40, 130, 260, scale, 8)
+    (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, 130, 260, scale, 8)
     up = torch.full_like(sa, 2.0 ** 60, dtype=torch.float32)
     sa, sb = (sa.float() * up).to(sa.dtype), (sb.float() * 2.0 ** -60).to(sb.dtype)
     want, mag = lowbit.matmul(av, sav, bv, sbv)
@@ -213,7 +214,7 @@ def test_matmul_extreme_scales(ctx, scale):
     assert (np.abs(lowbit.as_float64(got) - want) <= off_by(260, mag, want, torch.float32)).all()
 
 
-@pytest.mark.parametrize("m,n,k", [(1, 700, 1000), (300, 300, 400)])
+@pytest.mark.parametrize("m,n,k", [(1, 700, 1000), (300, 300, 400), (4200, 300, 400)])
 def test_matmul_same_bits_in_streams_and_graphs(ctx, m, n, k):
     (a, sa, _, _), (b, sb, _, _) = operands(m, n, k, "e8m0", 6)
     first = ctx.matmul_e4m3(a, sa, b, sb)
@@ -239,7 +240,7 @@ def test_matmul_same_bits_in_streams_and_graphs(ctx, m, n, k):
 
 def test_matmul_long_sums(ctx):
     """Many blocks of K: several parts of an accumulator, several chunks of scales, ends inside both."""
-    for m, n, k in ((130, 130, 4096 + 128 * 3 + 5), (20, 70, 20000), (257, 100, 12345)):
+    for m, n, k in ((130, 130, 4096 + 128 * 3 + 5), (20, 70, 20000), (257, 100, 12345), (2300, 515, 4096 + 200), (1030, 1030, 2600)):
         for scale in ("e8m0", "f32"):
             (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, n, k, scale, 2)
             want, mag = lowbit.matmul(av, sav, bv, sbv)
@@ -247,7 +248,7 @@ def test_matmul_long_sums(ctx):
             assert (np.abs(lowbit.as_float64(got) - want) <= off_by(k, mag, want, torch.float32)).all()
 
 
-@pytest.mark.parametrize("m", [30, 300])
+@pytest.mark.parametrize("m", [30, 300, 4200])
 def test_matmul_scale_that_is_no_number(ctx, m):
     """The byte 255 spoils its row's sums."""
     (a, sa, av, sav), (b, sb, bv, sbv) = operands(m, 140, 300, "e8m0", 4)
@@ -262,7 +263,7 @@ def test_matmul_scale_that_is_no_number(ctx, m):
 def test_two_graphs_and_an_eager_call(ctx):
     """Two captured products replayed in turn with a call in between: they share nothing."""
     sets = []
-    for seed, m in ((1, 20), (2, 300)):
+    for seed, m in ((1, 20), (2, 300), (3, 4200)):
         (a, sa, _, _), (b, sb, _, _) = operands(m, 200, 300, "e8m0", seed)
         out = ctx.matmul_e4m3(a, sa, b, sb)
         want = out.clone()
@@ -302,7 +303,7 @@ def test_binding_refuses(ctx):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("scale", ["e8m0", "f32"])
-@pytest.mark.parametrize("m", [40, 300])
+@pytest.mark.parametrize("m", [40, 300, 4200])
 @pytest.mark.parametrize("ldd", [256, 264, 260, 257, 258])
 def test_matmul_rows_that_begin_anywhere(ctx, m, ldd, dtype, scale):
     """Results whose rows begin on boundaries of 32 bytes, of 16 and of less, at the buffer's start and inside it."""

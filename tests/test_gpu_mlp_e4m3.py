@@ -165,13 +165,14 @@ def test_little_workspace(ctx):
     assert torch.equal(got, want)
 
 
-@pytest.mark.parametrize("m", [5, 300])
-def test_wait_that_runs_out(m):
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("m", [5, 300, 4200])
+def test_wait_that_runs_out(m, scale):
     """Copies that never come: the kernel gives up in bounded time, the call's status says so, and the next call is right."""
     c = ks.Context(DESC, 0)
     g = torch.Generator().manual_seed(2)
     a, b = torch.randn(m, 300, generator=g).to(DEV), torch.randn(200, 300, generator=g).to(DEV)
-    qa, qb = c.quantize_e4m3(a), c.quantize_e4m3(b, block_rows=128)
+    qa, qb = c.quantize_e4m3(a, scale=scale), c.quantize_e4m3(b, block_rows=128, scale=scale)
     want = c.matmul_e4m3(*qa, *qb)
     c.debug_set_wait(50, 1)
     c.matmul_e4m3(*qa, *qb)
