@@ -168,7 +168,7 @@ struct PairShared {  // behind the stages
   float b_scale[2][2][kChunk];
   float bias[2][kTile];
   Tile tile[2];
-  float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 16-byte boundaries
+  alignas(16) float store[16][32 * kStorePitch];  // of a warp, for results whose rows do not begin on 16-byte boundaries
   float amax[2][16][32];  // of a warp's rows, for the one that has the block's other half
 };
 constexpr int kSmem = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(PairShared));
@@ -214,9 +214,42 @@ __device__ __forceinline__ float block_max(const float (&sum)[kCols], bool& odd)
 }
 
 // Writes them, rounded to the result's type (e4m3: already scaled).
-template <int kType>
+template <int kType, bool kLines>
 __device__ __forceinline__ void store_block(const MatmulArgs& p, int row, int n0, const float (&sum)[kCols], bool odd, float* s_store) {
   const int lane = threadIdx.x & 31;
+  if constexpr (kLines && kType != KS_F32) {
+    // whole lines through shared memory, 1 KB at a time: a thread that writes its own row touches 32 lines a store (60,000 x 1,024 x
+    // 1,024, bf16: 73 us so, 66 by lines). Where the instructions of the sums bound the kernel it does not pay (e4m3: 86 and 92).
+    if (p.row_bytes > 0 && n0 + kCols <= p.n) {
+      constexpr int kRow = kCols * kBytes<kType>, kPieces = kRow / 16, kRows = 1024 / kRow, kPer = 4 / kBytes<kType>;
+      auto at = [](int r, int c) { return r * kRow + (c ^ (kPieces == 8 ? r & 7 : r >> 1 & 3)) * 16; };  // (no conflicts)
+      char* stage = reinterpret_cast<char*>(s_store);
+      char* out = static_cast<char*>(p.d) + (static_cast<int64_t>(row - lane) * p.ldd + n0) * kBytes<kType>;
+      uint32_t w[kRow / 4];
+#pragma unroll
+      for (int i = 0; i < kRow / 4; ++i) {
+        const float* v = sum + i * kPer;
+        if (kType == KS_E4M3 && !odd) w[i] = e4m3_pair_finite(v[0], v[1]) | (e4m3_pair_finite(v[2], v[3]) << 16);
+        else w[i] = pack<kType>(v);
+      }
+#pragma unroll
+      for (int g = 0; g < 32; g += kRows) {
+        __syncwarp();
+        if (lane / kRows == g / kRows)
+#pragma unroll
+          for (int c = 0; c < kPieces; ++c)
+            *reinterpret_cast<uint4*>(stage + at(lane % kRows, c)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 64; i += 32) {
+          const int r = (i + lane) / kPieces, c = lane % kPieces;
+          if (row - lane + g + r < p.m)
+            *reinterpret_cast<uint4*>(out + (g + r) * p.ldd * kBytes<kType> + c * 16) = *reinterpret_cast<const uint4*>(stage + at(r, c));
+        }
+      }
+      return;
+    }
+  }
   constexpr int kPer = 4 / kBytes<kType>;  // elements of four bytes
   // (rows on boundaries of 16 bytes, 20,357 x 4,340 x 1,230: fp32 322 us by threads that write their own row, 235 through shared
   // memory; bf16 197 and 201. Of 32 bytes, n = 4,352: 183 and 174, 151 and 201.)
@@ -492,7 +525,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 #pragma unroll
         for (int q = 0; q < kCols; ++q) sum[q] *= inv;
       }
-      if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
+      if (inside) store_block<kType, false>(p, row, n0, sum, odd, sh.store[warp - 4]);
     }
   }
   // after a failure: time for the copies and MMAs in flight to end
@@ -522,7 +555,7 @@ struct ScaledShared {  // behind the stages
   alignas(128) uint8_t scale[kScaleBuffers][kScaleBytes];
   alignas(16) float bias[2][kTile];
   Tile tile[2];
-  float store[16][32 * kStorePitch];
+  alignas(16) float store[16][32 * kStorePitch];
   float amax[2][16][32];
 };
 constexpr int kSmemScaled = 1024 + kStages * kStageBytes + static_cast<int>(sizeof(ScaledShared));
@@ -704,21 +737,25 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
       };
       for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u, ++tile_count) {
         const Tile at = tile_at(t, tiles_m, tiles_n);
+        float bias[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int n = at.n + j * kHalf + 32 * i + lane;
+          bias[i] = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f;
+        }
         if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_bias_read(tile_par), ((tile_count >> 1) & 1u) ^ 1u)))) break;
         if (j == 0 && lane == 0) sh.tile[tile_par] = at;
-        for (int i = 0; i < 4; ++i) {
-          const int n = j * kHalf + 32 * i + lane;
-          sh.bias[tile_par][n] = p.bias && at.n + n < p.n ? __ldg(p.bias + at.n + n) : 0.0f;
-        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sh.bias[tile_par][j * kHalf + 32 * i + lane] = bias[i];
         __syncwarp();
         if (lane == 0) bar_arrive(bar_bias(tile_par));
         const int row = at.m + static_cast<int>(rank) * kHalf + r0, nb = at.n / kScaleBlock + j;
         for (int kb = 0; kb < p.kblocks; kb += kWords) {
-          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_used(buf), parity_used)))) break;
-          const int n_kb = p.kblocks - kb;
+          const int n_kb = p.kblocks - kb;  // (loaded in front of the wait)
           const uint32_t w0 = row < p.m ? word_at(p.a_scale, static_cast<int64_t>(row) * p.kblocks + kb, n_kb) : 0u;
           const uint32_t w1 = row + 32 < p.m ? word_at(p.a_scale, static_cast<int64_t>(row + 32) * p.kblocks + kb, n_kb) : 0u;
           const uint32_t wb = nb * kScaleBlock < p.n ? word_at(p.b_scale, static_cast<int64_t>(nb) * p.kblocks + kb, n_kb) : 0u;
+          if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_used(buf), parity_used)))) break;
           uint32_t* out = reinterpret_cast<uint32_t*>(sh.scale[buf]);
           // row r of 128: 16 bytes a lane r % 32, word r / 32 of them
           out[lane * 4 + 2 * j] = w0;
@@ -784,7 +821,7 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
 #pragma unroll
         for (int q = 0; q < kCols; ++q) sum[q] *= inv;
       }
-      if (inside) store_block<kType>(p, row, n0, sum, odd, sh.store[warp - 4]);
+      if (inside) store_block<kType, true>(p, row, n0, sum, odd, sh.store[warp - 4]);
     }
   }
   // after a failure: time for the copies and MMAs in flight to end
