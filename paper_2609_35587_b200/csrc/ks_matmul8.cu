@@ -545,7 +545,8 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 // tile of K = 1,024 takes an SM in matmul_pair_kernel, 17,000 read the accumulators of its blocks. The tensor core adds by
 // truncation, so a part is 4,096 of K at most (128 additions, each off by 2^-24 at most), and the parts are added in registers.
 // The scales' places leave room for one accumulator: the MMAs stand still while it is read into registers, 700 clocks of the
-// 4,100 of K = 1,024, but not while a tile is finished and written.
+// 4,100 of K = 1,024, but not while a tile is finished and written. That takes about 6,000 clocks (60,000 x 1,024 results: 41 us
+// for K = 128 quantised, 45 as bf16, 74 as fp32), so up to K = 1,024 it bounds the kernel as much as the MMAs do.
 constexpr int kPart = 32;         // blocks of K that an accumulator takes
 constexpr int kWords = 4;         // blocks of K whose scales are in a word
 constexpr int kScaleBuffers = 4;
