@@ -191,8 +191,8 @@ ks_status ks_model_create_mlp(ks_ctx* ctx, int n_layers, const int* h_widths,
  * power of two as scale for each block of 128 x 128 (ks_quantize_e4m3 of the given bf16 weights, KS_SCALE_E8M0), and so are
  * the rows that a layer reads, with a scale for each row and 128 of its values: the standardised inputs x' in fp32, and
  * h = ReLU(W h_prev + b) of the fp32 sums of ks_matmul_e4m3. The last hidden layer is rounded to bf16 instead, and the last
- * layer is s = w . h + b in fp32 as above. For the shapes that are bound by the tensor cores: ks_score and the ks_select calls
- * serve it; ks_select holds at most 37,888 rows of activations at a time and 67 M scores. Synchronous. */
+ * layer is s = w . h + b in fp32 as above. A pair's score does not depend on the others of its call. For the shapes that are
+ * bound by the tensor cores: ks_score and the ks_select calls serve it; ks_select holds at most 37,888 rows of activations at a time and 67 M scores. Synchronous. */
 ks_status ks_model_create_mlp_e4m3(ks_ctx* ctx, int n_layers, const int* h_widths,
                                    const uint16_t* const* h_w_bf16, const float* const* h_bias,
                                    const float* h_mu, const float* h_sigma, ks_model** out_model);
@@ -395,8 +395,9 @@ ks_status ks_quantize_e4m3(ks_ctx* ctx, const void* d_x, int x_type, int64_t row
  *                   does the fp32 sums, scales of scale_type to d_d_scale [m][ceil(n / 128)]; d_d and ldd as d_q and ldq there
  *   d_d_scale       only for KS_E4M3, else NULL
  * The scales' products sa * sb have to be fp32 numbers; d_d may overlap none of the inputs. m == 0 or n == 0 does nothing;
- * k == 0 is the empty sum. The same call gives the same bits. Asynchronous on `stream`; no workspace. m, n, k <= KS_MAX_EXTENT;
- * KS_ERR_UNSUPPORTED where a grid would not hold them. */
+ * k == 0 is the empty sum. The same call gives the same bits; with KS_SCALE_E8M0, n and k <= KS_MLP_MAX_WIDTH a row's results do not
+ * depend on the other rows either (larger and KS_SCALE_F32 calls add in an order that goes by m). Asynchronous on `stream`; no
+ * workspace. m, n, k <= KS_MAX_EXTENT; KS_ERR_UNSUPPORTED where a grid would not hold them. */
 ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const void* d_a_scale, const uint8_t* d_b, int64_t ldb,
                          const void* d_b_scale, int scale_type, int64_t m, int64_t n, int64_t k, const float* d_bias, int relu,
                          void* d_d, int64_t ldd, int d_type, void* d_d_scale, void* stream);

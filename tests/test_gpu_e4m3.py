@@ -320,3 +320,17 @@ def test_matmul_rows_that_begin_anywhere(ctx, m, ldd, dtype, scale):
         left = flat.clone()
         left[start:start + m * ldd].view(m, ldd)[:, :n] = 7.0
         assert bool((left == 7).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("n,k", [(64, 64), (128, 256), (256, 80), (1024, 1024)])
+def test_matmul_rows_by_themselves(ctx, n, k, dtype):
+    """With powers of two and K up to 1,024 a row's result does not depend on the rows beside it."""
+    m = 4500
+    (a, sa, _, _), (b, sb, _, _) = operands(m, n, k, "e8m0", 11)
+    values_of = lambda r: [t.view(torch.uint8) for t in r] if dtype == torch.float8_e4m3fn else [r]  # noqa: E731
+    whole = values_of(ctx.matmul_e4m3(a, sa, b, sb, relu=True, out_dtype=dtype))
+    for first, rows in ((0, 1), (4321, 1), (100, 16), (7, 17), (300, 60), (511, 130), (0, 1000), (255, 4097)):
+        part = values_of(ctx.matmul_e4m3(a[first:first + rows], sa[first:first + rows], b, sb, relu=True, out_dtype=dtype))
+        for w, p in zip(whole, part):
+            assert torch.equal(w[first:first + rows], p), (first, rows)

@@ -181,3 +181,48 @@ def test_wait_that_runs_out(m, scale):
     assert torch.equal(c.matmul_e4m3(*qa, *qb), want)
     assert c.device_status() == ks.KS_OK
     c.close()
+
+
+@pytest.mark.parametrize("onehot,hidden", [(False, [128]), (True, [64]), (False, [256, 128]), (False, [192, 320]), (True, [1024, 1024, 512, 256])])
+def test_a_row_scores_the_same_whatever_is_beside_it(ctx, onehot, hidden):
+    """Alone, among a few, in a full batch, in the rest behind one, and with little workspace: equal bits."""
+    mlp = make(onehot, hidden, 9)
+    model = ctx.model_create_mlp_e4m3(mlp)
+    _, _, _, x = features(ctx, 4, 5000)
+    base = ctx.score(x, model)
+    for rows in (1, 16, 17, 65, 500, 4000):
+        for first in range(0, len(x), 2500):
+            part = x[first:first + rows].contiguous()
+            assert torch.equal(ctx.score(part, model), base[first:first + len(part)]), (rows, first)
+    at = torch.arange(BATCH + 2112, device=DEV) % len(x)
+    assert torch.equal(ctx.score(x[at], model), base[at])
+    small = ks.Context(DESC, 0)
+    model2 = small.model_create_mlp_e4m3(mlp)
+    small.debug_limit_workspace(8 << 20)
+    assert torch.equal(small.score(x[at], model2), base[at])
+    assert small.device_status() == ks.KS_OK
+    small.close()
+
+
+@pytest.mark.parametrize("hidden", [[128], [256, 128], [1024, 512]])
+def test_select_over_several_batches(ctx, hidden):
+    """Copies of the best candidates lie in the rest behind the first batch: they score the same, and the lower index comes first."""
+    k, rest = 32, 2112
+    model = ctx.model_create_mlp_e4m3(make(False, hidden, 10))
+    w = wl.make_workload(2, P=1, C=BATCH, trees=4, depth=2)
+    d_p, d_c = ks.to_device(w.problems, torch.device(DEV)), ks.to_device(w.candidates, torch.device(DEV))
+    first = ctx.score(ctx.featurize(d_p, 1, d_c, BATCH), model).cpu().numpy()
+    order = np.lexsort((np.arange(BATCH), -first))
+    pool = np.concatenate([w.candidates, w.candidates[order[:rest]]])
+    d_c = ks.to_device(pool, torch.device(DEV))
+    scores = ctx.score(ctx.featurize(d_p, 1, d_c, len(pool)), model).cpu().numpy()
+    np.testing.assert_array_equal(scores, np.concatenate([first, first[order[:rest]]]))
+    want = np.lexsort((np.arange(len(pool)), -scores))[:k]
+    for idx, sc in ((t.cpu().numpy() for t in ctx.select(d_p, 1, d_c, len(pool), model, k)),
+                    (t.cpu().numpy()[None] for t in ctx.select_one(w.problems[:1], d_c, len(pool), model, k))):
+        np.testing.assert_array_equal(idx[0], want)
+        np.testing.assert_array_equal(sc[0], scores[want])
+    few = order[:40]  # the same candidates as a small pool
+    idx, sc = (t.cpu().numpy() for t in ctx.select_one(w.problems[:1], ks.to_device(w.candidates[few], torch.device(DEV)), len(few), model, 8))
+    np.testing.assert_array_equal(sc, first[few][:8])
+    assert (first[few[idx]] == sc).all()
