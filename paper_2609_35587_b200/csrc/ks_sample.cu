@@ -1201,8 +1201,9 @@ cudaError_t launch_type(const SampleArgs& a, cudaStream_t stream, int64_t* launc
   const int64_t len = std::max<int64_t>(1, a.seg_off ? a.c / a.p : a.c);  // (of segments the mean)
   // Short rows by a warp each: all of a call, or those of many segments or of segments that are short on the average, in a launch of
   // their own (4,096 rows of 32 scores with top-k: 60 us by CTAs, 6 by warps; of 256 scores 60 and 26. Warps of the other
-  // kernel's CTAs instead of a launch: no gain, its code grows).
-  const bool all_short = a.c <= kShortRow, some_short = a.seg_off && (a.p >= kManyRows || len <= kShortRow);
+  // kernel's CTAs instead of a launch: no gain, its code grows). Of segments the offsets alone say how long they are, and a replayed
+  // graph may find others than the call was made with: both kernels follow, whatever their total is said to be.
+  const bool all_short = !a.seg_off && a.c <= kShortRow, some_short = a.seg_off && (a.p >= kManyRows || len <= kShortRow);
   if (all_short || some_short) {
     if (a.p > INT32_MAX) return cudaErrorInvalidConfiguration;
     const cudaError_t e = launch_following(&short_rows_kernel<T>, dim3(static_cast<unsigned>((a.p + kShortWarps - 1) / kShortWarps)),

@@ -283,3 +283,35 @@ def test_many_scores_around_the_cut(ctx, p, c, dtype, s, spread):
     idx, logp = draw(ctx, x, u, **s)
     for r in ([0] if p == 1 else [0, p - 1]):
         lowbit.check_draws(lowbit.as_float64(x[r]), u[r].cpu().numpy(), idx[r].cpu().numpy(), logp[r].cpu().numpy(), **s)
+
+
+def raw(ctx, scores, c, off, u, idx, logp, **s):
+    """The C call with a total of its own."""
+    one = ks._Sampling(s.get("t", 1.0), s.get("top_k", 0), s.get("top_p", 1.0), s.get("min_p", 0.0))
+    st = ks._lib.ks_sample(ctx._h, scores.data_ptr(), ks._TYPES[scores.dtype], u.shape[0], c, 0, off.data_ptr(), ks.ctypes.byref(one), None,
+                           u.data_ptr(), u.shape[1], idx.data_ptr(), logp.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert st == ks.KS_OK
+
+
+@pytest.mark.parametrize("c", [0, 1, 200, 256, 257, 10 ** 6])
+@pytest.mark.parametrize("s", [dict(), dict(top_k=9), dict(top_p=0.8, min_p=0.01)], ids=str)
+def test_total_of_segments_decides_no_draw(ctx, c, s):
+    """Rows are as long as the offsets say, whatever the call was told about their total; also where a replayed graph finds others."""
+    lens = [[3, 256, 0, 5, 90], [900, 0, 257, 5, 4000], [0, 0, 256, 60000, 1]]
+    x = (torch.randn(61000, generator=torch.Generator().manual_seed(21)) * 2).to(DEV)
+    offs = [torch.tensor([0] + n, dtype=torch.int64).cumsum(0).to(DEV) for n in lens]
+    u = numbers(5, 6, 4)
+    off = offs[0].clone()
+    idx, lp = torch.full((5, 6), 77, dtype=torch.int32, device=DEV), torch.full((5, 6), 77.0, device=DEV)
+    raw(ctx, x, c, off, u, idx, lp, **s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        raw(ctx, x, c, off, u, idx, lp, **s)
+    for o in offs:
+        off.copy_(o)
+        idx.fill_(77)
+        lp.fill_(77.0)
+        graph.replay()
+        check(x, u, idx, lp, rows=o.cpu().numpy(), **s)
+        want = ctx.sample(x, u, d_seg_off=o, **{{"t": "temperature"}.get(k, k): v for k, v in s.items()})
+        assert torch.equal(idx, want[0]) and torch.equal(lp, want[1])
