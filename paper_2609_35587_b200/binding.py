@@ -7,6 +7,7 @@ no CPU fallback: importing this module without the built library raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -143,6 +144,14 @@ def _dptr(t):
 
 # The operators' small calls take a few microseconds on the device: their arguments go to the library as plain integers.
 _raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _int32(v):
+    """A whole number as the library's 32-bit arguments hold it (ctypes would wrap it)."""
+    v = operator.index(v)
+    if not -1 << 31 <= v < 1 << 31:
+        raise ValueError(f"{v} does not fit 32 bits")
+    return v
 
 
 def _rows(t, device):
@@ -500,10 +509,11 @@ class Context:
         """Rows of fp32 / bf16 / fp16 values to e4m3 with a scale ("e8m0" or "f32") for each block of
         block_rows (1 or 128) x 128. Returns (q, scales); the rows of q begin on 16-byte boundaries."""
         rows, cols = x.shape
+        block_rows = _int32(int(block_rows))
         dev = self.device.index
         xp, ldx = _rows(x, dev)
         st, dtype = _SCALES[scale]
-        blocks = (-(-rows // max(int(block_rows), 1)), (cols + 127) // 128)  # an invalid one is reported by the library, not by torch
+        blocks = (-(-rows // max(block_rows, 1)), (cols + 127) // 128)  # an invalid one is reported by the library, not by torch
         if out is None:
             out = _empty_e4m3(x, rows, cols)
         elif out.shape != x.shape or out.dtype != torch.float8_e4m3fn:
@@ -513,7 +523,7 @@ class Context:
         elif out_scale.shape != blocks or out_scale.dtype != dtype:
             raise ValueError("quantize_e4m3: out_scale")
         qp, ldq = _rows(out, dev)
-        status = _lib.ks_quantize_e4m3(self._h, xp, _TYPES.get(x.dtype, -1), rows, cols, ldx, int(block_rows), st, qp, ldq,
+        status = _lib.ks_quantize_e4m3(self._h, xp, _TYPES.get(x.dtype, -1), rows, cols, ldx, block_rows, st, qp, ldq,
                                        _flat(out_scale, dev), _raw_stream(dev))
         if status:
             self._check(status, "ks_quantize_e4m3")
@@ -548,7 +558,7 @@ class Context:
             raise ValueError("matmul_e4m3: out_scale")
         op, ldd = _rows(out, dev)
         status = _lib.ks_matmul_e4m3(self._h, ap, lda, _flat(a_scale, dev), bp, ldb, _flat(b_scale, dev), _SCALE_TYPES[scales],
-                                     m, n, k, None if bias is None else _flat(bias, dev), int(relu), op, ldd,
+                                     m, n, k, None if bias is None else _flat(bias, dev), 1 if relu else 0, op, ldd,
                                      _TYPES.get(out_dtype, -1), _flat(out_scale, dev) if quantised else None, _raw_stream(dev))
         if status:
             self._check(status, "ks_matmul_e4m3")
@@ -560,7 +570,7 @@ class Context:
         numbers u [P, draws]. `params`: [P] SAMPLING_DT records on the device (to_device), settings of each row
         instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each; with an
         out_idx and no out_logp the second is None and not computed."""
-        P, draws = u.shape
+        P, draws = (_int32(n) for n in u.shape)
         dev = self.device.index
         up = _flat(u, dev)
         if u.dtype != torch.float32 or scores.dtype not in _TYPES:
@@ -584,7 +594,7 @@ class Context:
             raise ValueError("sample: out_idx")
         if out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32):
             raise ValueError("sample: out_logp")
-        one = None if params is not None else ctypes.byref(_Sampling(temperature, top_k, top_p, min_p))
+        one = None if params is not None else ctypes.byref(_Sampling(temperature, _int32(top_k), top_p, min_p))
         status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params, dev),
                                 up, draws, _flat(out_idx, dev), None if out_logp is None else _flat(out_logp, dev), _raw_stream(dev))
         if status:

@@ -126,3 +126,51 @@ def test_binding_wants_the_context_device():
             with pytest.raises(ValueError):
                 fn(t, 0)
         assert fn(there, 1)
+
+
+class Recorded:
+    """In the place of the library: what it is called with."""
+    call = None
+
+    def __getattr__(self, name):
+        def fn(*args):
+            self.call = (name, args)
+            return ks.KS_OK
+        return fn
+
+
+class Handle:
+    class device:
+        index = -1  # (of tensors in host memory)
+    _h = None
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    lib = Recorded()
+    monkeypatch.setattr(ks, "_lib", lib)
+    monkeypatch.setattr(ks, "_raw_stream", lambda device: 0)
+    return lib
+
+
+@pytest.mark.parametrize("v", [1 << 31, (1 << 32) + 1, (1 << 32) + 128, -(1 << 31) - 1, -(1 << 32) + 1])
+def test_numbers_that_32_bits_do_not_hold(recorded, v):
+    """They are refused: wrapped, block_rows would write more scales than the binding made room for, and top_k would be another."""
+    x, u = torch.zeros(4, 200), torch.zeros(4, 2)
+    with pytest.raises(ValueError):
+        ks.Context.quantize_e4m3(Handle, x, block_rows=v)
+    with pytest.raises(ValueError):
+        ks.Context.sample(Handle, x, u, top_k=v)
+    assert recorded.call is None
+
+
+def test_whole_numbers_of_other_types(recorded):
+    x, u = torch.zeros(4, 200), torch.zeros(4, 2)
+    ks.Context.quantize_e4m3(Handle, x, block_rows=np.int64(128))
+    assert recorded.call[1][6] == 128
+    ks.Context.sample(Handle, x, u, top_k=np.int64(7))
+    assert recorded.call[1][7]._obj.top_k == 7
+    q, s = torch.zeros(4, 128).to(torch.float8_e4m3fn), torch.zeros(4, 1)
+    for relu, want in ((1 << 32, 1), (True, 1), (0, 0)):
+        ks.Context.matmul_e4m3(Handle, q, s, q, s[:1], relu=relu)
+        assert recorded.call[1][12] == want
