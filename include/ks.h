@@ -410,9 +410,10 @@ ks_status ks_matmul_e4m3(ks_ctx* ctx, const uint8_t* d_a, int64_t lda, const voi
  * least top_p of theirs (at least one); of these those with w_j >= min_p. With s the sum of what stays, a draw for u in [0, 1) is
  * the first candidate in the order of the indices up to which the weights that stay sum to more than u s.
  * Temperature 0: the best candidate (the first of those that share the score), whatever u.
- *   d_scores       device, score_type KS_F32, KS_BF16 or KS_F16. Without d_seg_offsets row i is [i * ld, i * ld + c), ld >= c; with it
- *                  (P + 1 non-decreasing entries) row i is [d_seg_offsets[i], d_seg_offsets[i + 1]), c their total length (it
- *                  decides how the work is shared out, not what is drawn), and ld is not used. A row has at most KS_MAX_EXTENT scores
+ *   d_scores       device, score_type KS_F32, KS_BF16 or KS_F16; NULL with c == 0: no row has a score. Without d_seg_offsets row i is
+ *                  [i * ld, i * ld + c), ld >= c; with it (P + 1 non-decreasing entries) row i is [d_seg_offsets[i],
+ *                  d_seg_offsets[i + 1]), c about their total length (it decides how the work is shared out, not what is drawn), and
+ *                  ld is not used. A row has at most KS_MAX_EXTENT scores
  *   d_params       device, [P], settings of each row, or NULL: *h_params for all rows. Of d_params a temperature that is not
  *                  above 0 counts as 0, top_k < 1 as 0, top_p not below 1 as 1, min_p not above 0 as 0
  *   d_u            device, [P][draws] fp32; below 0 counts as 0, from 1 on as the largest below 1. 1 <= draws <= KS_MAX_K

@@ -912,7 +912,8 @@ ks_status ks_sample(ks_ctx* ctx, const void* d_scores, int score_type, int P, in
       !aligned(d_u, 4) || !aligned(d_idx, 4) || !aligned(d_logp, 4))
     return KS_ERR_INVALID_ARG;
   DeviceGuard g(ctx->device);
-  const ks::SampleArgs a{d_scores, ld, d_seg_offsets, P, c, d_params ? ks_sampling{} : *h_params, d_params, d_u, draws, d_idx, d_logp};
+  // (without scores nothing is read, whatever the offsets say)
+  const ks::SampleArgs a{d_scores, ld, d_scores ? d_seg_offsets : nullptr, P, c, d_params ? ks_sampling{} : *h_params, d_params, d_u, draws, d_idx, d_logp};
   cudaError_t e = ks::launch_sample(a, score_type, static_cast<cudaStream_t>(stream), &ctx->launches);
   if (e == cudaErrorInvalidConfiguration) return KS_ERR_UNSUPPORTED;
   return e == cudaSuccess ? KS_OK : cuda_fail(ctx, e, "ks_sample");

@@ -315,3 +315,12 @@ def test_total_of_segments_decides_no_draw(ctx, c, s):
         check(x, u, idx, lp, rows=o.cpu().numpy(), **s)
         want = ctx.sample(x, u, d_seg_off=o, **{{"t": "temperature"}.get(k, k): v for k, v in s.items()})
         assert torch.equal(idx, want[0]) and torch.equal(lp, want[1])
+
+
+def test_segments_without_scores(ctx):
+    """No scores at all (a tensor without elements has no address), though the offsets name some: nothing is read."""
+    none = torch.empty(0, device=DEV)
+    assert none.data_ptr() == 0
+    off = torch.tensor([0, 300, 300, 700], dtype=torch.int64, device=DEV)
+    idx, logp = ctx.sample(none, numbers(3, 2, 1), d_seg_off=off)
+    assert idx.tolist() == [[-1, -1]] * 3 and bool((logp == -np.inf).all())
