@@ -23,7 +23,7 @@ using Wide = unsigned long long;
 constexpr int kSms = 148;  // of the one device this library is built for
 
 __device__ __forceinline__ float scale_value(const void* s, int64_t at, int type) {
-  return type == KS_SCALE_E8M0 ? e8m0_value(__ldg(static_cast<const uint8_t*>(s) + at)) : __ldg(static_cast<const float*>(s) + at);
+  return type == KS_SCALE_E8M0 ? e8m0_value(static_cast<const uint8_t*>(s)[at]) : static_cast<const float*>(s)[at];
 }
 
 // sum += value * s for two neighbours
@@ -87,7 +87,7 @@ struct MatmulArgs {
 
 // Value of an element of the result before it is rounded.
 __device__ __forceinline__ float finish(const MatmulArgs& p, float v, int n) {
-  if (p.bias) v += __ldg(p.bias + n);
+  if (p.bias) v += p.bias[n];
   if (p.relu) v = v > 0.0f ? v : 0.0f;
   return v;
 }
@@ -431,7 +431,7 @@ matmul_pair_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int n = (warp - 2) * kHalf + 32 * i + lane;
-              sh.bias[tile_par][n] = at.n + n < p.n ? __ldg(p.bias + at.n + n) : 0.0f;
+              sh.bias[tile_par][n] = at.n + n < p.n ? p.bias[at.n + n] : 0.0f;
             }
           const int j = warp - 2, nb = at.n / kScaleBlock + j;
           float w = 0.0f;
@@ -729,11 +729,11 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
       const bool words = p.kblocks % kWords == 0 && reinterpret_cast<uintptr_t>(p.a_scale) % 4 == 0 && reinterpret_cast<uintptr_t>(p.b_scale) % 4 == 0;
       auto word_at = [&](const void* scales, int64_t at, int n_kb) {
         const uint8_t* from = static_cast<const uint8_t*>(scales) + at;
-        if (words) return __ldg(reinterpret_cast<const uint32_t*>(from));
+        if (words) return *reinterpret_cast<const uint32_t*>(from);
         uint32_t w = 0;
 #pragma unroll
         for (int k = 0; k < kWords; ++k)
-          if (k < n_kb) w |= static_cast<uint32_t>(__ldg(from + k)) << (8 * k);
+          if (k < n_kb) w |= static_cast<uint32_t>(from[k]) << (8 * k);
         return w;
       };
       for (uint32_t t = pair; t < tiles && ok; t += n_pairs, tile_par ^= 1u, ++tile_count) {
@@ -742,7 +742,7 @@ matmul_scaled_kernel(const __grid_constant__ MatmulArgs p, const __grid_constant
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int n = at.n + j * kHalf + 32 * i + lane;
-          bias[i] = p.bias && n < p.n ? __ldg(p.bias + n) : 0.0f;
+          bias[i] = p.bias && n < p.n ? p.bias[n] : 0.0f;
         }
         if (!(ok = __all_sync(0xFFFFFFFFu, wait_ok(bar_bias_read(tile_par), ((tile_count >> 1) & 1u) ^ 1u)))) break;
         if (j == 0 && lane == 0) sh.tile[tile_par] = at;

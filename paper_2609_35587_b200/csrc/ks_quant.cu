@@ -29,7 +29,7 @@ __device__ __forceinline__ void store_scale(void* scale, int64_t at, uint32_t st
 template <typename T, int N, bool kVec>
 __device__ __forceinline__ void load_values(const T* row, int64_t c, int64_t cols, float (&v)[N]) {
   if (kVec && c + N <= cols) {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + c));
+    const uint4 w = *reinterpret_cast<const uint4*>(row + c);
     T t[N];
     static_assert(sizeof(t) == 16, "one load");
     memcpy(t, &w, 16);

@@ -469,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
   const uint32_t inner = last >= static_cast<uint32_t>(shift) + V ? last - shift - V + 1 : 0;
 
   auto fetch = [&](uint32_t at) KS_INLINE {
-    return at - shift < inner ? __ldg(reinterpret_cast<const uint4*>(base + at)) : fetch_edge(base, at, shift, last);
+    return at - shift < inner ? *reinterpret_cast<const uint4*>(base + at) : fetch_edge(base, at, shift, last);
   };
   // Place of a load: those of a warp are neighbours, and warps follow one another in a tile.
   auto place = [&](int tile, int w, int q) KS_INLINE {

@@ -130,7 +130,8 @@ __device__ __forceinline__ void tmem_read32(uint32_t taddr, uint32_t (&r)[32]) {
       : "memory");
 }
 // The operators' kernels follow one another as programmatic dependents: the next one's blocks are set up while this one's last
-// still run. Nothing of global memory is touched in front of the wait.
+// still run. Nothing of global memory is touched in front of the wait, and behind it nothing is loaded through the read-only path
+// (__ldg), which promises that memory stays as it is from the kernel's first block on, while the kernels in front still write it.
 __device__ __forceinline__ void next_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

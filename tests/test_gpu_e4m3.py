@@ -334,3 +334,39 @@ def test_matmul_rows_by_themselves(ctx, n, k, dtype):
         part = values_of(ctx.matmul_e4m3(a[first:first + rows], sa[first:first + rows], b, sb, relu=True, out_dtype=dtype))
         for w, p in zip(whole, part):
             assert torch.equal(w[first:first + rows], p), (first, rows)
+
+
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("m,n,k", [(8, 512, 2048), (100, 300, 256), (2300, 300, 256)])
+def test_buffers_written_again_by_calls_that_follow_at_once(ctx, m, n, k, scale):
+    """Operands, sums and draws in the same buffers, call after call: kernels that begin while those in front end read what these wrote."""
+    times = 40
+    xs = [values(m, k, 50 + i) for i in range(3)]
+    b, sb = ctx.quantize_e4m3(values(n, k, 7) / 64, block_rows=128, scale=scale)
+    u = torch.rand(m, 2, generator=torch.Generator().manual_seed(1)).to(DEV)
+
+    def one(x):
+        q, s = ctx.quantize_e4m3(x, scale=scale)
+        d = ctx.matmul_e4m3(q, s, b, sb, out_dtype=torch.float32)
+        torch.cuda.synchronize()
+        return (d, *ctx.sample(d, u, temperature=50.0))
+    want = [one(x) for x in xs]
+    q, s = ctx.quantize_e4m3(xs[0], scale=scale)
+    d = torch.empty(m, n, device=DEV)
+    got = [(torch.empty_like(want[0][1]), torch.empty_like(want[0][2])) for _ in range(times)]
+
+    def chain():
+        for i, (idx, logp) in enumerate(got):
+            ctx.quantize_e4m3(xs[i % 3], scale=scale, out=q, out_scale=s)
+            ctx.matmul_e4m3(q, s, b, sb, out_dtype=torch.float32, out=d)
+            ctx.sample(d, u, temperature=50.0, out_idx=idx, out_logp=logp)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        chain()
+    for run in (chain, graph.replay, graph.replay):
+        for idx, logp in got:
+            idx.fill_(-7)
+        run()
+        for i, (idx, logp) in enumerate(got):
+            assert torch.equal(idx, want[i % 3][1]) and torch.equal(logp, want[i % 3][2]), i
+        assert torch.equal(d, want[(times - 1) % 3][0])

@@ -1,6 +1,8 @@
 """What ks_quantize_e4m3, ks_matmul_e4m3 and ks_sample refuse, without a GPU: arguments are checked before the context is used,
 so a block of zeros stands in for one, and no pointer is followed."""
 import ctypes
+import os
+import re
 
 import numpy as np
 import pytest
@@ -174,3 +176,13 @@ def test_whole_numbers_of_other_types(recorded):
     for relu, want in ((1 << 32, 1), (True, 1), (0, 0)):
         ks.Context.matmul_e4m3(Handle, q, s, q, s[:1], relu=relu)
         assert recorded.call[1][12] == want
+
+
+def test_dependent_kernels_load_what_the_one_in_front_wrote():
+    """The operators' kernels begin while the one in front still writes: no load through the read-only path, which may be moved or kept."""
+    csrc = os.path.join(os.path.dirname(ks.__file__), "csrc")
+    dependents = [f for f in sorted(os.listdir(csrc)) if "  wait_for_last();" in open(os.path.join(csrc, f)).read()]
+    assert dependents == ["ks_matmul8.cu", "ks_quant.cu", "ks_sample.cu"]
+    for f in dependents + ["ks_e4m3.cuh"]:
+        code = re.sub(r"//.*", "", open(os.path.join(csrc, f)).read())
+        assert not re.search(r"__ldg|ld\.global\.nc|__restrict__", code), f
