@@ -370,3 +370,45 @@ def test_buffers_written_again_by_calls_that_follow_at_once(ctx, m, n, k, scale)
         for i, (idx, logp) in enumerate(got):
             assert torch.equal(idx, want[i % 3][1]) and torch.equal(logp, want[i % 3][2]), i
         assert torch.equal(d, want[(times - 1) % 3][0])
+
+
+def quantised(x, block_rows, scale):
+    q, s = lowbit.quantize(lowbit.as_float64(x), block_rows, scale)
+    qt = torch.zeros(x.shape[0], -(-x.shape[1] // 16) * 16)
+    qt[:, :x.shape[1]] = torch.from_numpy(q)
+    dt = torch.float8_e8m0fnu if scale == "e8m0" else torch.float32
+    return qt.to(torch.float8_e4m3fn).to(DEV)[:, :x.shape[1]], torch.from_numpy(s).float().to(dt).to(DEV), q, s
+
+
+@pytest.mark.parametrize("signs", [False, True])
+@pytest.mark.parametrize("scale", [torch.float32, torch.float8_e8m0fnu])
+@pytest.mark.parametrize("m,n,k", [(40, 130, 1024), (1700, 515, 1024), (40, 130, 8192), (1700, 515, 4096), (1700, 260, 16384)])
+def test_matmul_sums_that_24_bits_hold(ctx, m, n, k, scale, signs):
+    """Values 1, 1.125, .. 1.875 with scales 1: products are multiples of 2^-6 below 4, a sum of 16,384 of them has 22 bits. Sums of
+    24 bits are exact, in any order, rounded or cut; sums of fewer are not."""
+    g = torch.Generator(device=DEV).manual_seed(k)
+
+    def some(rows):
+        v = 1 + torch.randint(0, 8, (rows, k), generator=g, device=DEV) / 8
+        return v * (1 - 2 * torch.randint(0, 2, (rows, k), generator=g, device=DEV)) if signs else v
+    a, b = some(m), some(n)
+    sa, sb = torch.ones(m, k // 128, device=DEV).to(scale), torch.ones(-(-n // 128), k // 128, device=DEV).to(scale)
+    got = ctx.matmul_e4m3(a.to(torch.float8_e4m3fn), sa, b.to(torch.float8_e4m3fn), sb, out_dtype=torch.float32)
+    assert torch.equal(got.double(), a.double() @ b.double().t())
+
+
+@pytest.mark.parametrize("positive", [False, True])
+@pytest.mark.parametrize("scale", ["e8m0", "f32"])
+@pytest.mark.parametrize("m,n,k", [(40, 300, 1000), (1700, 515, 1000), (40, 300, 4296), (1700, 515, 4096), (1700, 515, 4296)])
+def test_matmul_error_goes_with_the_additions(ctx, m, n, k, scale, positive):
+    """An addition of the tensor core takes 32 of K: it cuts the sum below a unit of its 24 bits, and what it cuts off the 32 products
+    is no more than another. The kernel with scales of two in its tiles adds k / 32 times (and a part of 4,096 of K to the next with one rounding);
+    the others four times within a block, then a block with roundings of the scales' product and of the sum, and up to eight parts."""
+    x, y = values(m, k, 31), values(n, k, 32)
+    (a, sa, av, sav), (b, sb, bv, sbv) = (quantised(v.abs() if positive else v, r, scale) for v, r in ((x, 1), (y, 128)))
+    want, mag = lowbit.matmul(av, sav, bv, sbv)
+    got = lowbit.as_float64(ctx.matmul_e4m3(a, sa, b, sb, out_dtype=torch.float32))
+    blocks = lowbit.blocks_of(k)
+    in_tiles = scale == "e8m0" and (m > 1000 or (n <= 1024 and k <= 1024))
+    units = 2 * -(-k // 32) + 1 if in_tiles else 8 + blocks / 2 + 2 + 4
+    assert (np.abs(got - want) <= units * 2.0 ** -23 * mag).all(), (np.abs(got - want) / mag).max() * 2.0 ** 23
