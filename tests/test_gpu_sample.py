@@ -324,3 +324,37 @@ def test_segments_without_scores(ctx):
     off = torch.tensor([0, 300, 300, 700], dtype=torch.int64, device=DEV)
     idx, logp = ctx.sample(none, numbers(3, 2, 1), d_seg_off=off)
     assert idx.tolist() == [[-1, -1]] * 3 and bool((logp == -np.inf).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("mean", ["short", "long"])
+@pytest.mark.parametrize("s", [None, dict(t=0.8, top_p=0.9), dict(top_k=60), dict()], ids=str)
+def test_many_segments(ctx, dtype, mean, s):
+    """As many segments as a CTA each takes: short ones of a launch of their own, ones that are kept on chip, ones that are not, and (long on
+    the average) none that are; settings of the call or of each row."""
+    p = 400
+    rng = np.random.RandomState(5)
+    lens = np.exp(rng.uniform(0, np.log(1500), p)).astype(np.int64)
+    lens[rng.rand(p) < 0.05] = 0
+    lens[:12] = [255, 256, 257, 258, 511, 512, 513, 1024, 1025, 7169, 14337, 30000]
+    if mean == "long":
+        lens[20:80] = rng.randint(60000, 140000, 60)
+    rng.shuffle(lens)
+    rows = np.concatenate([[0], np.cumsum(lens)])
+    x = (torch.randn(int(rows[-1]), generator=torch.Generator().manual_seed(31)) * 2).to(dtype)
+    x[torch.rand(len(x), generator=torch.Generator().manual_seed(32)) < 0.05] = -float("inf")
+    x, u, off = x.to(DEV), numbers(p, 5, 33), torch.from_numpy(rows).to(DEV)
+    if s is None:
+        rec = np.zeros(p, ks.SAMPLING_DT)
+        rec["temperature"], rec["top_k"] = rng.uniform(0.3, 2.0, p), rng.randint(0, 200, p)
+        rec["top_p"], rec["min_p"] = rng.uniform(0.3, 1.1, p), rng.uniform(-0.05, 0.05, p)
+        rec["temperature"][rng.rand(p) < 0.1] = 0.0
+        idx, logp = draw(ctx, x, u, seg_off=off, params=ks.to_device(rec, DEV))
+        settings = [dict(t=r["temperature"], top_k=int(r["top_k"]), top_p=min(r["top_p"], 1.0), min_p=max(r["min_p"], 0.0)) for r in rec]
+    else:
+        idx, logp = draw(ctx, x, u, seg_off=off, **s)
+        settings = [s] * p
+    xs, un, i, lp = lowbit.as_float64(x), u.cpu().numpy(), idx.cpu().numpy(), logp.cpu().numpy()
+    for r in range(p):
+        if lens[r] < 20000 or r % 8 == 0:
+            lowbit.check_draws(xs[rows[r]:rows[r + 1]], un[r], i[r], lp[r], **settings[r])
