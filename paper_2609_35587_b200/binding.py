@@ -570,7 +570,9 @@ class Context:
         numbers u [P, draws]. `params`: [P] SAMPLING_DT records on the device (to_device), settings of each row
         instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each; with an
         out_idx and no out_logp the second is None and not computed."""
-        P, draws = (_int32(n) for n in u.shape)
+        P, draws = u.shape
+        if P >= 1 << 31 or draws >= 1 << 31:  # (ctypes would wrap them)
+            raise ValueError("sample: sizes of u")
         dev = self.device.index
         up = _flat(u, dev)
         if u.dtype != torch.float32 or scores.dtype not in _TYPES:

@@ -186,3 +186,11 @@ def test_dependent_kernels_load_what_the_one_in_front_wrote():
     for f in dependents + ["ks_e4m3.cuh"]:
         code = re.sub(r"//.*", "", open(os.path.join(csrc, f)).read())
         assert not re.search(r"__ldg|ld\.global\.nc|__restrict__", code), f
+
+
+@pytest.mark.parametrize("shape", [(1, (1 << 32) + 1), ((1 << 32) + 3, 1), (1 << 31, 2)])
+def test_more_draws_than_32_bits_count(recorded, shape):
+    u = torch.zeros(1).expand(shape)  # (one number's memory)
+    with pytest.raises(ValueError, match="sizes of u"):
+        ks.Context.sample(Handle, torch.zeros(1, 5).expand(shape[0], 5), u)
+    assert recorded.call is None
