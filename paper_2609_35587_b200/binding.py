@@ -7,7 +7,6 @@ no CPU fallback: importing this module without the built library raises.
 from __future__ import annotations
 
 import ctypes
-import operator
 import os
 
 import numpy as np
@@ -144,14 +143,7 @@ def _dptr(t):
 
 # The operators' small calls take a few microseconds on the device: their arguments go to the library as plain integers.
 _raw_stream = torch._C._cuda_getCurrentRawStream
-
-
-def _int32(v):
-    """A whole number as the library's 32-bit arguments hold it (ctypes would wrap it)."""
-    v = operator.index(v)
-    if not -1 << 31 <= v < 1 << 31:
-        raise ValueError(f"{v} does not fit 32 bits")
-    return v
+_INT_MAX = (1 << 31) - 1  # (ctypes wraps what 32 bits do not hold)
 
 
 def _rows(t, device):
@@ -509,7 +501,9 @@ class Context:
         """Rows of fp32 / bf16 / fp16 values to e4m3 with a scale ("e8m0" or "f32") for each block of
         block_rows (1 or 128) x 128. Returns (q, scales); the rows of q begin on 16-byte boundaries."""
         rows, cols = x.shape
-        block_rows = _int32(int(block_rows))
+        block_rows = int(block_rows)
+        if not -_INT_MAX <= block_rows <= _INT_MAX:
+            raise ValueError("quantize_e4m3: block_rows")
         dev = self.device.index
         xp, ldx = _rows(x, dev)
         st, dtype = _SCALES[scale]
@@ -571,8 +565,10 @@ class Context:
         instead of the call's. Returns (positions in the row, log of their probability), [P, draws] each; with an
         out_idx and no out_logp the second is None and not computed."""
         P, draws = u.shape
-        if P >= 1 << 31 or draws >= 1 << 31:  # (ctypes would wrap them)
+        if P > _INT_MAX or draws > _INT_MAX:
             raise ValueError("sample: sizes of u")
+        if not -_INT_MAX <= top_k <= _INT_MAX:
+            raise ValueError("sample: top_k")
         dev = self.device.index
         up = _flat(u, dev)
         if u.dtype != torch.float32 or scores.dtype not in _TYPES:
@@ -596,7 +592,7 @@ class Context:
             raise ValueError("sample: out_idx")
         if out_logp is not None and (out_logp.shape != u.shape or out_logp.dtype != torch.float32):
             raise ValueError("sample: out_logp")
-        one = None if params is not None else ctypes.byref(_Sampling(temperature, _int32(top_k), top_p, min_p))
+        one = None if params is not None else ctypes.byref(_Sampling(temperature, top_k, top_p, min_p))
         status = _lib.ks_sample(self._h, sp, _TYPES[scores.dtype], P, c, ld, off, one, None if params is None else _flat(params, dev),
                                 up, draws, _flat(out_idx, dev), None if out_logp is None else _flat(out_logp, dev), _raw_stream(dev))
         if status:
