@@ -386,8 +386,8 @@ ks_status ks_quantize_e4m3(ks_ctx* ctx, const void* d_x, int x_type, int64_t row
 
 /* d[i][j] = act(sum over blocks b of 128 of sa[i][b] * sb[j / 128][b] * (sum over k in b of a[i][k] * b[j][k]) + bias[j]) for
  * i < m, j < n, with fp32 sums (KS_SCALE_E8M0: the tensor core adds 32 of K at a time, which cuts a sum off towards zero, by up to
- * 2^-23 of it, and does so for up to 4,096 of K; what it adds to is fp32), rounded once to d_type: a layer on rows held in eight bits with weights [n][k] held in eight
- * bits. act is the identity or, with `relu`, x for x > 0 and else 0.
+ * 2^-23 of it, and does so for up to 4,096 of K; what it adds to is fp32), rounded once to d_type: a layer on rows held in eight
+ * bits with weights [n][k] held in eight bits. act is the identity or, with `relu`, x for x > 0 and else 0.
  *   d_a, d_b        device, e4m3, [m][k] and [n][k], rows lda / ldb bytes apart; 16-byte aligned, lda and ldb multiples of 16
  *   d_a_scale       device, [m][ceil(k / 128)] of scale_type (ks_quantize_e4m3 with block_rows 1)
  *   d_b_scale       device, [ceil(n / 128)][ceil(k / 128)] of scale_type (block_rows 128)

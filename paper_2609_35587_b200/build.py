@@ -2,7 +2,7 @@
 
 Every .cu file is compiled to an object of its own (in parallel) under build/, then linked.
 ``build(debug=True)`` makes libks_debug.so instead: the same sources with KS_DEBUG_BOUNDS
-defined, in which the kernels range-check the indices they form from data and record the
+defined, in which the tree kernels range-check the indices they form from data and record the
 first violation in a word the host can read (``ks_debug_bounds_line``) instead of touching
 memory out of range.
 """

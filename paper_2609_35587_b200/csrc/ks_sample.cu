@@ -22,9 +22,11 @@
 // (short rows by four CTAs an SM), others read again in every phase by two CTAs an SM, which is what stays in L2. Rows of up to
 // 256 scores belong to a warp each (short_rows_kernel).
 //
-// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 350 us where reading them takes 38: three passes, of
+// What bounds it: instructions. 1,024 x 60,000 fp32 scores with top-p take 357 us where reading them takes 38: three passes, of
 // which the one with the weights (20 operations in 64 bits and the sums) takes half; the issue slots are 66 % busy, the fp64
-// pipe 12 %. With top-k 50 113 us. Few rows are bound by the phases' latency: one of 60,000 scores 12 us with top-k, 33 with top-p.
+// pipe 12 %. With top-k 50 110 us, without cuts 195. The phases are one kernel of 64 registers a thread, for 1,024 threads an SM, which
+// spills (fp32 scores 88 bytes of stores and 120 of loads, 16-bit ones 312 and 572). Few rows are bound by the phases' latency: one of
+// 60,000 scores 12 us with top-k, 29 with top-p.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
